@@ -64,8 +64,9 @@ def sources_hash():
     import hashlib
     h = hashlib.sha256()
     for f in sorted(glob.glob(os.path.join(ROOT, "paper_2411_19114_amd", "csrc", "*"))):
-        # the image path's sources (the audio path and the batching server have no part in it)
-        if f.endswith((".hip", ".cpp", ".h")) and os.path.basename(f) not in ("audio.hip", "audio_plan.h", "batcher.cpp"):
+        # the image path's sources (the audio path, the batching server and the batches of tokens have no part in it)
+        if f.endswith((".hip", ".cpp", ".h")) and os.path.basename(f) not in ("audio.hip", "audio_plan.h", "batcher.cpp", "patches.hip", "packing.hip",
+                                                                               "rotary.hip", "tokens.h"):
             h.update(os.path.basename(f).encode())
             with open(f, "rb") as fh:
                 h.update(fh.read())

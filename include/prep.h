@@ -419,6 +419,208 @@ int64_t prep_audio_frames(const prep_audio_config *cfg, uint64_t samples_in, int
 int prep_audio_features(prep_audio *h, const float *waveforms, const uint64_t *offsets, int32_t n,
                         int32_t rate_in, float *out, uint64_t *out_offsets, void *stream);
 
+/* ---- batches for language models that read images and video ----------------------
+ *
+ * What such a model takes in place of a fixed crop: every image at a size of its own, cut
+ * into patches, a row a patch, the rows of a batch packed without padding (prep_patch_rows,
+ * prep_decode_patches_batch); the place of every token on three axes (time, height, width;
+ * prep_token_positions); its queries and keys rotated by these places (prep_rotary_*); and
+ * where in a paged cache the batch's tokens go (prep_block_slots).
+ *
+ * These calls (prep_decode_patches_batch excepted, which follows prep_decode_resize_batch) take
+ * a device ordinal or a handle that belongs to one device, leave the caller's current device as
+ * it was, enqueue on `stream`, allocate no device memory and wait for nothing, and may be
+ * captured into a HIP graph.  Lengths that are DEVICE arrays are read when the work runs, so a
+ * captured call follows them.  Two calls may run at the same time unless they write the same
+ * memory.  Pointers are aligned as what they point to, else PREP_E_INVALID_ARG.
+ */
+enum { PREP_BF16 = 3 };    /* a third element type, of these calls only            */
+
+/* Patch rows.  An image is resized as a whole to a height and a width that are multiples of
+ * patch * merge: the multiples nearest to its own size (halves upwards, at least one); if
+ * that holds more than max_pixels pixels, the largest multiples not above side *
+ * sqrt(max_pixels / pixels of the image), at least one; else, if it holds fewer than
+ * min_pixels, the smallest not below side * sqrt(min_pixels / pixels of the image).
+ * Then (v / 255 - mean[c]) / std[c].  A row holds frames_per_patch frames of one patch as
+ * [3][frames_per_patch][patch][patch]; the rows of a clip come frame group by frame group,
+ * in a group window by window (merge x merge patches, windows in raster order, patches in
+ * raster order inside), so that merge * merge rows in a row make one token of a model that
+ * merges them.  The last frame stands in for frames that the last group lacks. */
+typedef struct {
+    int32_t patch;             /* 1..64                                             */
+    int32_t merge;             /* 1..16                                             */
+    int32_t frames_per_patch;  /* 1..16; a still is a clip of one frame             */
+    int32_t out_dtype;         /* PREP_F32, PREP_F16 or PREP_BF16                   */
+    float mean[3], std[3];     /* on the 0..1 pixel scale, R, G, B                  */
+    int32_t filter;            /* PREP_FILTER_BILINEAR or PREP_FILTER_ANTIALIAS     */
+    int32_t reserved;          /* 0                                                 */
+    int64_t min_pixels, max_pixels; /* >= 0; 0 = no bound                           */
+} prep_patch_params;
+
+/* Patches of one clip: grid[0] frame groups of grid[1] rows of grid[2] patches (HOST).
+ * PREP_E_INVALID_ARG where a side would exceed 65535 pixels.                       */
+int prep_patch_grid(const prep_patch_params *params, int32_t width, int32_t height, int32_t frames, int32_t grid[3]);
+
+/*
+ * Patch rows of n clips of decoded frames.
+ *   rgb      DEVICE  interleaved 8-bit RGB frames; frame f of clip i starts at byte rgb_offsets[i] +
+ *            f * frame_strides[i], rows are pitches[i] bytes apart; nothing outside the rows' own
+ *            3 * width bytes is read
+ *   rgb_offsets, widths, heights, pitches   HOST, n entries each
+ *   frames, frame_strides   HOST, n entries each; both NULL = stills
+ *   out      DEVICE  rows out_stride elements apart (0 = without gaps), room for out_rows of them;
+ *            what lies between rows and behind the last one is left as it was
+ *   row_starts  HOST, n + 1 entries, written by the call: clip i has rows row_starts[i] up to
+ *            row_starts[i + 1].  PREP_E_TOO_LARGE, and nothing enqueued, if out_rows is fewer.
+ */
+int prep_patch_rows(int32_t device, const uint8_t *rgb, const uint64_t *rgb_offsets, const int32_t *widths,
+                    const int32_t *heights, const int32_t *pitches, const int32_t *frames,
+                    const uint64_t *frame_strides, int32_t n, const prep_patch_params *params, void *out,
+                    int64_t out_stride, int64_t out_rows, int64_t *row_starts, void *stream);
+
+/*
+ * The same from JPEG files: prep_decode_resize_batch (or, with bitstreams_device, ..._resident) with patch
+ * rows in place of the fixed crop.  A file whose headers are refused has no rows; one that turns
+ * out corrupt on the GPU has rows of zeros (prep_get_status tells).  The handle's rules are those
+ * of prep_decode_resize_batch.
+ */
+int prep_decode_patches_batch(prep_handle *h, const uint8_t *bitstreams, const uint8_t *bitstreams_device,
+                              const uint64_t *offsets, int32_t n, const prep_patch_params *params, void *out,
+                              int64_t out_stride, int64_t out_rows, int64_t *row_starts, void *stream);
+
+/* A piece of a sequence.  Text of n tokens is {n, 0, 0, 0}; an image or a clip of t frames of h x w
+ * tokens is {t, h, w, step}, each 0..32767 and h, w >= 1.  Anything else counts as no tokens.
+ * A sequence's places start at p = first[i].  Text token j has p + j on all three axes, and p moves
+ * on by n.  Token (a, y, x) of a grid has p + a * step, p + y, p + x, and p moves on by
+ * max((t - 1) * step, h - 1, w - 1) + 1 (not at all if t is 0).  Tokens of a grid come frame by frame, in a
+ * frame in raster order, or with merge > 1 window by window as patch rows do (windows of merge x merge, cut at
+ * the edge). */
+typedef struct {
+    int32_t t, h, w, step;
+} prep_segment;
+
+/*
+ * Places of a packed batch's tokens.
+ *   segments      DEVICE  n_segments records, at most 1048576
+ *   seq_segments  DEVICE  n_seq + 1 entries, ascending: sequence i has segments seq_segments[i] up to
+ *                 seq_segments[i + 1] (values are clamped to 0..n_segments; segments of no sequence count for nothing)
+ *   first         DEVICE  n_seq entries, or NULL = 0
+ *   positions     DEVICE  [3][capacity]: token by token, sequence after sequence; 0 behind the last token;
+ *                 tokens beyond capacity are not written
+ *   token_starts  DEVICE  n_seq + 1 entries: first token of every sequence, and their number in all (which may
+ *                 exceed capacity; at most 2^31 - 1 is reported)
+ *   next          DEVICE  n_seq entries, or NULL: the place of the token that would follow each sequence
+ *   workspace     DEVICE  16-byte aligned, at least prep_token_positions_workspace(n_segments) bytes, of this call
+ *                 alone until it has run
+ * Places are computed modulo 2^32.  n_seq <= 65535.
+ */
+uint64_t prep_token_positions_workspace(int32_t n_segments);
+int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n_segments, const int32_t *seq_segments,
+                         int32_t n_seq, const int32_t *first, int32_t merge, int32_t *positions, int64_t capacity,
+                         int32_t *token_starts, int32_t *next, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Slots of a batch's new tokens in a paged cache of n_blocks blocks of block_size tokens.
+ * Request i has cached[i] tokens in the cache and fresh[i] new ones, which take the places behind them.
+ * A place p lies in the block table[i][p / block_size].  Blocks that a request lacks are taken
+ * from the stack of free blocks, in the order of the requests and of their places; the top of the stack is
+ * free_blocks[*free_count - 1].
+ *   cached, fresh  DEVICE, n entries each
+ *   free_blocks    DEVICE, room for free_capacity entries; free_count  DEVICE, one entry (more than free_capacity
+ *                  counts as free_capacity); neither is written
+ *   table          DEVICE, n rows of table_width entries, table_stride apart: the entries of the blocks
+ *                  taken are written, the others left as they were
+ *   slots          DEVICE, capacity entries: block * block_size + p mod block_size token by token, request
+ *                  after request; -1 for tokens of refused requests, for tokens whose block is not
+ *                  in 0..n_blocks-1, and behind the last token
+ *   token_starts   DEVICE, n + 1 entries: first token of every request, and their number (at most 2^31 - 1)
+ *   lengths        DEVICE, n entries: tokens of the request in the cache afterwards
+ *   status         DEVICE, n entries: PREP_OK; PREP_E_INVALID_ARG (a negative length; the request then
+ *                  has no tokens and length 0); PREP_E_TOO_LARGE: the request lacks blocks or its row of the
+ *                  table or `slots` ends too early; it takes no block and its length stays (requests
+ *                  behind one that the stack could not serve get no block either; those that need none are served)
+ *   free_left      DEVICE, one entry, another than free_count: blocks left on the stack.  A caller that keeps
+ *                  the stack passes it as the next call's free_count.
+ *   workspace      as above, prep_block_slots_workspace(n) bytes
+ */
+typedef struct {
+    int32_t n;                 /* requests, 0..1048576                              */
+    int32_t block_size;        /* 1..65536                                          */
+    int64_t n_blocks;          /* 0..2^31 - 1                                       */
+    const int32_t *cached, *fresh;
+    const int32_t *free_blocks;
+    int32_t free_capacity, table_width;
+    const int32_t *free_count;
+    int32_t *table;
+    int64_t table_stride;      /* >= table_width                                    */
+    int64_t capacity;          /* 0..2^31 - 1                                       */
+    int64_t *slots;
+    int32_t *token_starts, *lengths, *status, *free_left;
+    void *workspace;
+    uint64_t workspace_bytes;
+} prep_block_args;
+uint64_t prep_block_slots_workspace(int32_t n);
+int prep_block_slots(int32_t device, const prep_block_args *args, void *stream);
+
+/* Rotary embedding by places on one to three axes.  Of a head's head_dim values the first 2 * n are
+ * rotated, n = sections[0] + sections[1] + sections[2] pairs of them by the places on axis 0, 1 and 2:
+ * pair (a, b) -> (a cos u - b sin u, a sin u + b cos u), u = place * f, the others pass through.
+ *   pairing : PREP_PAIR_HALVES: pair i = values i and i + n; PREP_PAIR_ADJACENT: values 2i and 2i + 1
+ *   order   : which pairs an axis has.  PREP_SECTIONS_BLOCKS: the first sections[0] pairs axis 0, and so on;
+ *             PREP_SECTIONS_INTERLEAVED: pair i with i mod 3 = 1, i < 3 sections[1] axis 1; i mod 3 = 2,
+ *             i < 3 sections[2] axis 2; the others axis 0 (the sections must come out)
+ *   f       : frequencies[i] (HOST, n entries, radians a place) if given; else base^(-i / n); with
+ *             PREP_ROTARY_PER_AXIS base^(-j / sections[axis]) for the axis' j-th pair
+ * The angle is taken in 64-bit fixed point, modulo a turn, so it is as exact at place 2^30 as at
+ * place 1; sums are fp32, rounded once to the element type. */
+enum { PREP_PAIR_HALVES = 0, PREP_PAIR_ADJACENT = 1 };
+enum { PREP_SECTIONS_BLOCKS = 0, PREP_SECTIONS_INTERLEAVED = 1 };
+enum { PREP_ROTARY_PER_AXIS = 1 };
+typedef struct {
+    int32_t device;
+    int32_t head_dim;          /* 2..1024                                           */
+    int32_t sections[3];       /* >= 0, sum 1..head_dim / 2                         */
+    int32_t dtype;             /* PREP_F32, PREP_F16 or PREP_BF16                   */
+    int32_t pairing, order;
+    uint32_t flags;            /* 0 or PREP_ROTARY_PER_AXIS                         */
+    int32_t reserved;          /* 0                                                 */
+    double base;               /* > 0; not looked at where frequencies is given     */
+    const double *frequencies; /* finite, or NULL                                   */
+} prep_rotary_config;
+typedef struct prep_rotary prep_rotary;
+
+/* DEVICE elements [token][head][head_dim]: strides in elements, the last axis without gaps. */
+typedef struct {
+    void *data;
+    int64_t token_stride, head_stride;
+} prep_heads;
+
+typedef struct {
+    int64_t n_tokens;          /* >= 0                                              */
+    const int32_t *positions;  /* DEVICE: axis a of token i at [a * axis_stride + i] */
+    int64_t axis_stride;
+    prep_heads q, q_out;       /* q_heads heads, rotated from q to q_out            */
+    prep_heads k, k_out;       /* k_heads heads; k_out.data may be NULL with a cache */
+    prep_heads v;              /* k_heads heads, copied into the cache              */
+    int32_t q_heads, k_heads;  /* >= 0 each, not both 0                             */
+    int32_t inverse;           /* 1: rotate by -u, which is also the way back: the gradient with respect to
+                                  the input, given the one with respect to the output */
+    int32_t block_size;
+    /* A paged cache, or k_cache = v_cache = NULL.  Rotated k and v of token i go to slot slots[i]:
+     * element block * block_stride + offset * slot_stride + head * cache_head_stride with
+     * block = slot / block_size, offset = slot mod block_size.  Slots outside 0..n_blocks * block_size - 1
+     * (padding has -1) are not stored.  Slots that are stored must differ from one another. */
+    void *k_cache, *v_cache;
+    int64_t n_blocks, block_stride, slot_stride, cache_head_stride;
+    const int64_t *slots;      /* DEVICE, n_tokens entries                          */
+} prep_rotary_args;
+
+int prep_rotary_create(prep_rotary **out, const prep_rotary_config *cfg);
+int prep_rotary_destroy(prep_rotary *r);
+/* Outputs may be their inputs (the same pointer and strides); apart from that, what is read and what
+ * is written must not overlap.  A handle may be used by several threads and streams at once, and a call leaves nothing in it. */
+int prep_rotary_apply(prep_rotary *r, const prep_rotary_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,16 +7,20 @@ import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
-_SOURCES = ["entropy.hip", "reconstruct.hip", "resize.hip", "static_entry.hip", "api.cpp", "parser.cpp", "batcher.cpp", "audio.hip"]
+_SOURCES = ["entropy.hip", "reconstruct.hip", "resize.hip", "static_entry.hip", "api.cpp", "parser.cpp", "batcher.cpp", "audio.hip",
+            "patches.hip", "packing.hip", "rotary.hip"]
 
 OK, E_INVALID_ARG, E_TOO_LARGE, E_HIP, E_UNSUPPORTED, E_CORRUPT, E_NOMEM = 0, -1, -2, -3, -4, -5, -6
-F32, F16, U8_NHWC = 0, 1, 2
+F32, F16, U8_NHWC, BF16 = 0, 1, 2, 3
 FLAG_TABLES_PER_WORKGROUP = 1
 FLAG_FULL_RGB = 2
 FLAG_SMOOTH_CHROMA = 4
 FLAG_LARGE_WINDOWS = 8
 FILTER_BILINEAR, FILTER_ANTIALIAS = 0, 1
 STREAM_WHOLE, STREAM_WINDOWS, STREAM_UNJOINED = 0, 1, 2
+PAIR_HALVES, PAIR_ADJACENT = 0, 1
+SECTIONS_BLOCKS, SECTIONS_INTERLEAVED = 0, 1
+ROTARY_PER_AXIS = 1
 
 
 def lib_path():
@@ -61,6 +65,37 @@ class AudioConfig(C.Structure):
                 ("max_total_samples", C.c_uint64)]
 
 
+class PatchParams(C.Structure):
+    _fields_ = [("patch", C.c_int32), ("merge", C.c_int32), ("frames_per_patch", C.c_int32), ("out_dtype", C.c_int32),
+                ("mean", C.c_float * 3), ("std", C.c_float * 3), ("filter", C.c_int32), ("reserved", C.c_int32),
+                ("min_pixels", C.c_int64), ("max_pixels", C.c_int64)]
+
+
+class BlockArgs(C.Structure):
+    _fields_ = [("n", C.c_int32), ("block_size", C.c_int32), ("n_blocks", C.c_int64), ("cached", C.c_void_p), ("fresh", C.c_void_p),
+                ("free_blocks", C.c_void_p), ("free_capacity", C.c_int32), ("table_width", C.c_int32), ("free_count", C.c_void_p),
+                ("table", C.c_void_p), ("table_stride", C.c_int64), ("capacity", C.c_int64), ("slots", C.c_void_p),
+                ("token_starts", C.c_void_p), ("lengths", C.c_void_p), ("status", C.c_void_p), ("free_left", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class RotaryConfig(C.Structure):
+    _fields_ = [("device", C.c_int32), ("head_dim", C.c_int32), ("sections", C.c_int32 * 3), ("dtype", C.c_int32),
+                ("pairing", C.c_int32), ("order", C.c_int32), ("flags", C.c_uint32), ("reserved", C.c_int32), ("base", C.c_double),
+                ("frequencies", C.POINTER(C.c_double))]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RotaryArgs(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("positions", C.c_void_p), ("axis_stride", C.c_int64), ("q", Heads), ("q_out", Heads),
+                ("k", Heads), ("k_out", Heads), ("v", Heads), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("inverse", C.c_int32),
+                ("block_size", C.c_int32), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("n_blocks", C.c_int64),
+                ("block_stride", C.c_int64), ("slot_stride", C.c_int64), ("cache_head_stride", C.c_int64), ("slots", C.c_void_p)]
+
+
 class ServerConfig(C.Structure):
     _fields_ = [("handle", Config), ("params", Params), ("n_consumers", C.c_int32), ("batch_max", C.c_int32),
                 ("time_queue_us", C.c_int64), ("max_request_bytes", C.c_int32), ("queue_capacity", C.c_int32)]
@@ -95,6 +130,8 @@ EXPORTS = [
     "prep_server_submit", "prep_server_next", "prep_server_release", "prep_server_next_many",
     "prep_server_release_many", "prep_server_copy_tensor",
     "prep_audio_create", "prep_audio_destroy", "prep_audio_frames", "prep_audio_features",
+    "prep_patch_grid", "prep_patch_rows", "prep_decode_patches_batch", "prep_token_positions_workspace", "prep_token_positions",
+    "prep_block_slots_workspace", "prep_block_slots", "prep_rotary_create", "prep_rotary_destroy", "prep_rotary_apply",
 ]
 
 _lib = None
@@ -162,6 +199,21 @@ def lib():
         L.prep_audio_frames.argtypes = [C.POINTER(AudioConfig), C.c_uint64, C.c_int32]
         L.prep_audio_frames.restype = C.c_int64
         L.prep_audio_features.argtypes = [vp, vp, u64p, C.c_int32, C.c_int32, vp, u64p, vp]
+        i64p = C.POINTER(C.c_int64)
+        L.prep_patch_grid.argtypes = [C.POINTER(PatchParams), C.c_int32, C.c_int32, C.c_int32, i32p]
+        L.prep_patch_rows.argtypes = [C.c_int32, vp, u64p, i32p, i32p, i32p, i32p, u64p, C.c_int32, C.POINTER(PatchParams), vp,
+                                      C.c_int64, C.c_int64, i64p, vp]
+        L.prep_decode_patches_batch.argtypes = [vp, u8p, vp, u64p, C.c_int32, C.POINTER(PatchParams), vp, C.c_int64, C.c_int64, i64p, vp]
+        L.prep_token_positions_workspace.argtypes = [C.c_int32]
+        L.prep_token_positions_workspace.restype = C.c_uint64
+        L.prep_token_positions.argtypes = [C.c_int32, vp, C.c_int32, vp, C.c_int32, vp, C.c_int32, vp, C.c_int64, vp, vp, vp,
+                                           C.c_uint64, vp]
+        L.prep_block_slots_workspace.argtypes = [C.c_int32]
+        L.prep_block_slots_workspace.restype = C.c_uint64
+        L.prep_block_slots.argtypes = [C.c_int32, C.POINTER(BlockArgs), vp]
+        L.prep_rotary_create.argtypes = [C.POINTER(vp), C.POINTER(RotaryConfig)]
+        L.prep_rotary_destroy.argtypes = [vp]
+        L.prep_rotary_apply.argtypes = [vp, C.POINTER(RotaryArgs), vp]
         _lib = L
     return _lib
 
@@ -266,6 +318,15 @@ class Preprocessor:
         _check(lib().prep_decode_resize_batch_resident(
             self._h, bp, C.c_void_p(bitstreams_device_ptr), op, len(o) - 1, C.byref(params),
             C.c_void_p(out_ptr), C.c_void_p(stream)), "prep_decode_resize_batch_resident")
+
+    def decode_patches_batch(self, bitstreams, offsets, params, out_ptr, out_rows, out_stride=0, bitstreams_device_ptr=0, stream=0):
+        """prep_decode_patches_batch: JPEG files to patch rows; returns where each file's rows begin, and their number."""
+        b, bp = _u8(bitstreams)
+        o, op = _u64(offsets)
+        starts = (C.c_int64 * len(o))()
+        _check(lib().prep_decode_patches_batch(self._h, bp, bitstreams_device_ptr, op, len(o) - 1, C.byref(params), out_ptr, out_stride,
+                                               out_rows, starts, stream), "prep_decode_patches_batch")
+        return list(starts)
 
     def get_status(self, n):
         st = (C.c_int32 * max(n, 1))()
@@ -440,3 +501,96 @@ class AudioPreprocessor:
         if self._h:
             lib().prep_audio_destroy(self._h)
             self._h = C.c_void_p()
+
+
+# ---- batches for language models that read images and video ----------------------------------------
+
+
+def _list(kind, values):
+    values = values.tolist() if isinstance(values, np.ndarray) else values
+    return (kind * len(values))(*values)
+
+
+def make_patch_params(patch, merge, frames_per_patch, out_dtype, mean, std, filter=FILTER_BILINEAR, min_pixels=0, max_pixels=0):
+    p = PatchParams()
+    p.patch, p.merge, p.frames_per_patch = int(patch), int(merge), int(frames_per_patch)
+    p.out_dtype = {"f32": F32, "f16": F16, "bf16": BF16}.get(out_dtype, out_dtype)
+    p.filter, p.min_pixels, p.max_pixels = int(filter), int(min_pixels), int(max_pixels)
+    p.mean[:] = [float(m) for m in mean]
+    p.std[:] = [float(s) for s in std]
+    return p
+
+
+def patch_grid(params, width, height, frames=1):
+    """prep_patch_grid -> (frame groups, rows, columns) of a clip's patches."""
+    grid = (C.c_int32 * 3)()
+    _check(lib().prep_patch_grid(C.byref(params), int(width), int(height), int(frames), grid), "prep_patch_grid")
+    return tuple(grid)
+
+
+def patch_rows(device, rgb_ptr, rgb_offsets, widths, heights, pitches, params, out_ptr, out_rows, frames=None, frame_strides=None,
+               out_stride=0, stream=0):
+    """prep_patch_rows: patch rows of decoded frames; returns where each clip's rows begin, and their number."""
+    n = len(widths)
+    starts = (C.c_int64 * (n + 1))()
+    _check(lib().prep_patch_rows(
+        device, rgb_ptr, _list(C.c_uint64, rgb_offsets), _list(C.c_int32, widths), _list(C.c_int32, heights), _list(C.c_int32, pitches),
+        None if frames is None else _list(C.c_int32, frames), None if frame_strides is None else _list(C.c_uint64, frame_strides), n,
+        C.byref(params), out_ptr, out_stride, out_rows, starts, stream), "prep_patch_rows")
+    return list(starts)
+
+
+def token_positions_workspace(n_segments):
+    return int(lib().prep_token_positions_workspace(n_segments))
+
+
+def token_positions(segments_ptr, n_segments, seq_segments_ptr, n_seq, first_ptr, merge, positions_ptr, capacity, token_starts_ptr,
+                    next_ptr, workspace_ptr, workspace_bytes, device=0, stream=0):
+    """prep_token_positions: places of a packed batch's tokens on three axes, from device arrays."""
+    _check(lib().prep_token_positions(device, segments_ptr, n_segments, seq_segments_ptr, n_seq, first_ptr, merge, positions_ptr, capacity,
+                                      token_starts_ptr, next_ptr, workspace_ptr, workspace_bytes, stream), "prep_token_positions")
+
+
+def block_slots_workspace(n):
+    return int(lib().prep_block_slots_workspace(n))
+
+
+def block_slots(n, block_size, n_blocks, cached_ptr, fresh_ptr, free_blocks_ptr, free_capacity, free_count_ptr, table_ptr, table_stride,
+                table_width, slots_ptr, capacity, token_starts_ptr, lengths_ptr, status_ptr, free_left_ptr, workspace_ptr, workspace_bytes,
+                device=0, stream=0):
+    """prep_block_slots: block tables and slot map of a batch's new tokens, from device arrays."""
+    args = BlockArgs(n, block_size, n_blocks, cached_ptr, fresh_ptr, free_blocks_ptr, free_capacity, table_width, free_count_ptr, table_ptr,
+                     table_stride, capacity, slots_ptr, token_starts_ptr, lengths_ptr, status_ptr, free_left_ptr, workspace_ptr, workspace_bytes)
+    _check(lib().prep_block_slots(device, C.byref(args), stream), "prep_block_slots")
+
+
+class Rotary:
+    """prep_rotary_*: rotary embedding by places on up to three axes.  Tensors are (pointer, token stride, head stride)."""
+
+    def __init__(self, head_dim, sections, base, dtype, pairing=PAIR_HALVES, order=SECTIONS_BLOCKS, per_axis=False, frequencies=None, device=0):
+        cfg = RotaryConfig(device, head_dim, (C.c_int32 * 3)(*sections), {"f32": F32, "f16": F16, "bf16": BF16}.get(dtype, dtype), pairing, order,
+                           ROTARY_PER_AXIS if per_axis else 0, 0, float(base or 0.0), None)
+        if frequencies is not None:
+            cfg.frequencies = _list(C.c_double, [float(f) for f in frequencies])
+            if len(frequencies) != sum(sections):
+                raise PrepError(E_INVALID_ARG, "prep_rotary_create")
+        self._h = C.c_void_p()
+        _check(lib().prep_rotary_create(C.byref(self._h), C.byref(cfg)), "prep_rotary_create")
+
+    def apply(self, n_tokens, positions, axis_stride, q=(0, 0, 0), q_out=(0, 0, 0), q_heads=0, k=(0, 0, 0), k_out=(0, 0, 0), k_heads=0,
+              v=(0, 0, 0), inverse=False, k_cache=0, v_cache=0, n_blocks=0, block_size=0, block_stride=0, slot_stride=0, cache_head_stride=0,
+              slots=0, stream=0):
+        args = RotaryArgs(n_tokens, positions, axis_stride, q, q_out, k, k_out, v, q_heads, k_heads, 1 if inverse else 0, block_size, k_cache,
+                          v_cache, n_blocks, block_stride, slot_stride, cache_head_stride, slots)
+        _check(lib().prep_rotary_apply(self._h, C.byref(args), stream), "prep_rotary_apply")
+
+    def close(self):
+        if self._h:
+            lib().prep_rotary_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

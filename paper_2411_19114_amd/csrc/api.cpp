@@ -365,9 +365,10 @@ struct StreamCut {
     uint32_t row_bytes() const { return short_rows && total <= kStreamTinyBytes ? kStreamTinyRowBytes : kStreamRowBytes; }
 };
 
-// Parse every file and lay the batch out in the workspace.
+// Parse every file and lay the batch out in the workspace.  With a stage of its own (which takes whole
+// images) params is not looked at.
 int plan_batch(prep_handle *h, const uint8_t *bits, const uint64_t *offsets, int32_t n,
-               const prep_params *params, Plan *plan)
+               const prep_params *params, OutputStage *stage, Plan *plan)
 {
     h->parsed.resize((size_t)n);
     h->recs.resize((size_t)n);
@@ -436,7 +437,8 @@ int plan_batch(prep_handle *h, const uint8_t *bits, const uint64_t *offsets, int
             R.restart_interval = (uint16_t)I.restart_interval;
             R.sampling = (uint8_t)I.sampling;
             R.blocks_per_mcu = (uint8_t)I.blocks_per_mcu;
-            if (!make_resize_rec(I.width, I.height, params, R.rgb_off, R.rgb_pitch, &Z)) {
+            if (!(stage ? stage->add(i, I.width, I.height, R.rgb_off, R.rgb_pitch)
+                        : make_resize_rec(I.width, I.height, params, R.rgb_off, R.rgb_pitch, &Z))) {
                 // the crop window does not fit this image after resizing
                 I.status = R.status = PREP_E_UNSUPPORTED;
                 R.n_streams = 0;
@@ -448,7 +450,7 @@ int plan_batch(prep_handle *h, const uint8_t *bits, const uint64_t *offsets, int
             const int per = recon_mcus_per_group(I.sampling);
             const int mcu_w = 8 * luma_h(I.sampling), mcu_h = 8 * luma_v(I.sampling);
             int x_lo = 0, x_hi = I.width - 1, y_lo = 0, y_hi = I.height - 1;
-            if (!(h->cfg.flags & PREP_FLAG_FULL_RGB)) {
+            if (!stage && !(h->cfg.flags & PREP_FLAG_FULL_RGB)) {
                 const auto span = params->filter == PREP_FILTER_ANTIALIAS ? window_span : tap_span;
                 span(Z.off_x, Z.scale_x, params->crop_w, I.width, &x_lo, &x_hi);
                 span(Z.off_y, Z.scale_y, params->crop_h, I.height, &y_lo, &y_hi);
@@ -502,6 +504,10 @@ int plan_batch(prep_handle *h, const uint8_t *bits, const uint64_t *offsets, int
     if (P.n_blocks > h->cap_blocks || P.rgb_bytes > h->cap_rgb || P.n_windows > h->cap_windows ||
         P.n_streams > h->cap_streams)
         return PREP_E_TOO_LARGE;
+    if (stage) {
+        const int rc = stage->ready();
+        if (rc != PREP_OK) return rc;
+    }
     *plan = P;
     return PREP_OK;
 }
@@ -520,9 +526,9 @@ int take_slot(prep_handle *h, Slot **out)
 
 int run_batch(prep_handle *h, const uint8_t *bits_host, const uint8_t *bits_dev,
               const uint64_t *offsets, int32_t n, const prep_params *params, void *out,
-              hipStream_t stream, const int16_t *coef_host, uint64_t n_coef)
+              hipStream_t stream, const int16_t *coef_host, uint64_t n_coef, OutputStage *stage = nullptr)
 {
-    if (!h || !bits_host || !offsets || !out || n < 0 || !params_ok(params)) return PREP_E_INVALID_ARG;
+    if (!h || !bits_host || !offsets || n < 0 || (!stage && (!out || !params_ok(params)))) return PREP_E_INVALID_ARG;
     if (n > h->cfg.max_batch) return PREP_E_TOO_LARGE;
     h->last_n = 0;
     if (n == 0) return PREP_OK;
@@ -544,7 +550,7 @@ int run_batch(prep_handle *h, const uint8_t *bits_host, const uint8_t *bits_dev,
     if (rc != PREP_OK) return rc;
     CopyPool *pool = !bits_dev && total >= kPooledCopyBytes && total <= h->cap_bits ? CopyPool::get() : nullptr;
     const bool pooled = pool && pool->start(s->h_bits, base_host, total);
-    rc = plan_batch(h, base_host, rel.data(), n, params, &P);
+    rc = plan_batch(h, base_host, rel.data(), n, params, stage, &P);
     if (rc == PREP_OK && coef_host && n_coef != P.n_blocks * 64) rc = PREP_E_INVALID_ARG;
     if (pooled) pool->wait();
     if (rc != PREP_OK) return rc;
@@ -604,9 +610,13 @@ int run_batch(prep_handle *h, const uint8_t *bits_host, const uint8_t *bits_dev,
     launch_reconstruct(d_bits, s->d_recs, reinterpret_cast<const uint32_t *>(s->d_recs + n), n, P.recon_wgs,
                        P.groups_per_wg, h->d_coef, h->d_rgb, h->d_chroma, P.max_region_pixels, stream);
     if (timing) HIP_TRY(hipEventRecord(ev[3], stream));
-    launch_resize_normalize(h->d_rgb, s->d_rr, h->d_status, n, params->crop_h, params->crop_w,
-                            params->out_dtype, params->filter, s->h_rr, params->mean,
-                            params->std, out, true, stream);
+    int stage_rc = PREP_OK;
+    if (stage)
+        stage_rc = stage->launch(h->d_rgb, h->d_status, stream);
+    else
+        launch_resize_normalize(h->d_rgb, s->d_rr, h->d_status, n, params->crop_h, params->crop_w,
+                                params->out_dtype, params->filter, s->h_rr, params->mean,
+                                params->std, out, true, stream);
     if (timing) HIP_TRY(hipEventRecord(ev[4], stream));
     HIP_TRY(hipGetLastError());
     HIP_TRY(hipEventRecord(s->done, stream));
@@ -615,10 +625,20 @@ int run_batch(prep_handle *h, const uint8_t *bits_host, const uint8_t *bits_dev,
     h->last_n = n;
     h->last_decoded = !coef_host;
     h->last_stream = stream;
-    return PREP_OK;
+    return stage_rc;
 }
 
 }  // namespace
+
+namespace prep {
+
+int decode_batch(prep_handle *h, const uint8_t *bits_host, const uint8_t *bits_dev, const uint64_t *offsets,
+                 int32_t n, OutputStage *stage, hipStream_t stream)
+{
+    return run_batch(h, bits_host, bits_dev, offsets, n, nullptr, nullptr, stream, nullptr, 0, stage);
+}
+
+}  // namespace prep
 
 extern "C" {
 

@@ -57,6 +57,23 @@ void launch_resize_normalize(const uint8_t *rgb, const ResizeRec *rr, const int3
                              const ResizeRec *host_rr, const float mean[3], const float std[3], void *out,
                              bool wide_reads, hipStream_t stream);
 
+// api.cpp: a batch decoded like prep_decode_resize_batch's, with something else in place of its last stage.
+struct OutputStage {
+    // Image `image` of the batch lies w x h at byte src_off of the workspace, rows pitch bytes apart; false =
+    // the stage cannot take it (its status is then PREP_E_UNSUPPORTED).  In the order of the images; those whose
+    // headers are refused are left out.
+    virtual bool add(int32_t image, int w, int h, uint64_t src_off, uint32_t pitch) = 0;
+    // All images are added; an error ends the call with nothing enqueued.
+    virtual int ready() = 0;
+    // status: DEVICE, one entry an image.  Rows of an image may be read kRgbSlack bytes past their end.
+    virtual int launch(const uint8_t *rgb, const int32_t *status, hipStream_t stream) = 0;
+
+protected:
+    ~OutputStage() = default;
+};
+int decode_batch(prep_handle *h, const uint8_t *bits_host, const uint8_t *bits_dev, const uint64_t *offsets,
+                 int32_t n, OutputStage *stage, hipStream_t stream);
+
 // api.cpp: host-side checks and geometry shared by the entry points
 bool params_ok(const prep_params *p);
 // Mapping constants of one image (source offset and row pitch in bytes); false when the crop

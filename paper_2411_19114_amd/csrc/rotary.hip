@@ -1,0 +1,277 @@
+// Rotary embedding of queries and keys by places on up to three axes, with the store of keys and
+// values into a paged cache (gfx950).
+//
+// A pair (a, b) of a head becomes (a cos u - b sin u, a sin u + b cos u) with u = place * f.  The angle is formed as a
+// 64-bit fraction of a turn, place * (f / 2 pi * 2^64) modulo 2^64: the multiplication wraps exactly where
+// the angle does, so a far place loses nothing, and the two top bits are the quadrant.
+#include <hip/hip_runtime.h>
+#include <cmath>
+#include <stdint.h>
+
+#include <new>
+
+#include "../../include/prep.h"
+#include "tokens.h"
+
+struct prep_rotary {
+    int32_t device, head_dim, pairs, dtype, pairing;
+    uint64_t *d_turns;  // per pair: turns a place, as a fraction of 2^64; the two lowest bits hold the axis (2^-62 of a
+                        // turn, 2^-31 at the farthest place, below an fp32 angle's last bit)
+};
+
+namespace prep {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTrig = 1024;  // angles of a workgroup
+constexpr int kMaxTokens = 8;  // tokens of a workgroup
+
+struct RotaryShape {
+    int32_t head_dim, pairs;
+    int32_t tokens;  // of a workgroup
+};
+
+// cos and sin of a fraction of a turn.  Reduced to an eighth of a turn either side of a quadrant's middle
+// axis; there Taylor's series up to x^9 and x^10 leave 2e-9 and 1.2e-10.
+__device__ __forceinline__ float2 cos_sin(uint64_t phase)
+{
+    const uint32_t turn = (uint32_t)((phase + 0x80000000ull) >> 32);
+    const uint32_t quadrant = (turn + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(turn - (quadrant << 30)) * 1.4629180792671596e-9f;  // 2 pi / 2^32
+    const float z = x * x;
+    const float s = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), 1.0f);
+    const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
+    const bool swap = (quadrant & 1u) != 0;
+    const float a = swap ? s : c, b = swap ? c : s;
+    float2 r;
+    r.x = ((quadrant + 1u) & 2u) != 0 ? -a : a;
+    r.y = (quadrant & 2u) != 0 ? -b : b;
+    return r;
+}
+
+// Where the cache has token i's row, in elements, or -1.
+__device__ __forceinline__ int64_t cache_row(const prep_rotary_args &A, int64_t i)
+{
+    const int64_t slot = A.slots[i];
+    if (slot < 0 || slot >= A.n_blocks * A.block_size) return -1;
+    const int64_t block = slot / A.block_size;
+    return block * A.block_stride + (slot - block * A.block_size) * A.slot_stride;
+}
+
+// Any alignment and any number of pairs: one thread a pair, or a value behind the rotated ones.
+template <typename T, bool kHalves>
+__global__ __launch_bounds__(kThreads) void rotary_pairs(prep_rotary_args A, RotaryShape S, const uint64_t *__restrict__ turns)
+{
+    __shared__ float2 trig[kTrig];
+    const int64_t token0 = (int64_t)blockIdx.x * S.tokens;
+    const int n = (int)min((int64_t)S.tokens, A.n_tokens - token0);
+    for (int e = threadIdx.x; e < n * S.pairs; e += kThreads) {
+        const int t = e / S.pairs, p = e - t * S.pairs;
+        const uint64_t f = turns[p];
+        const int64_t place = A.positions[(int64_t)(f & 3u) * A.axis_stride + token0 + t];
+        float2 cs = cos_sin((uint64_t)place * (f & ~(uint64_t)3));
+        if (A.inverse) cs.y = -cs.y;
+        trig[e] = cs;
+    }
+    __syncthreads();
+    const bool store = A.k_cache != nullptr;
+    const int units = S.head_dim - S.pairs;  // pairs, then single values
+    const int heads = A.q_heads + A.k_heads * (store ? 2 : 1);
+    for (int e = threadIdx.x; e < n * heads * units; e += kThreads) {
+        const int row = e / units, u = e - row * units;
+        const int t = row / heads, head = row - t * heads;
+        const int64_t i = token0 + t;
+        const bool paired = u < S.pairs;
+        const int ia = paired && !kHalves ? 2 * u : paired ? u : u + S.pairs, ib = kHalves ? u + S.pairs : 2 * u + 1;
+        const int of_k = head - A.q_heads, of_v = of_k - A.k_heads;
+        const prep_heads &in = of_k < 0 ? A.q : of_v < 0 ? A.k : A.v;
+        const int h = of_k < 0 ? head : of_v < 0 ? of_k : of_v;
+        const T *src = (const T *)in.data + i * in.token_stride + (int64_t)h * in.head_stride;
+        T a = src[ia], b = paired ? src[ib] : a;
+        if (paired && of_v < 0) {
+            const float2 cs = trig[t * S.pairs + u];
+            const float x = to_float(a), y = to_float(b);
+            a = from_float<T>(fmaf(x, cs.x, -y * cs.y));
+            b = from_float<T>(fmaf(x, cs.y, y * cs.x));
+        }
+        if (of_v < 0) {
+            const prep_heads &out = of_k < 0 ? A.q_out : A.k_out;
+            if (out.data != nullptr) {
+                T *dst = (T *)out.data + i * out.token_stride + (int64_t)h * out.head_stride;
+                dst[ia] = a;
+                if (paired) dst[ib] = b;
+            }
+        }
+        if (store && of_k >= 0) {
+            const int64_t at = cache_row(A, i);
+            if (at >= 0) {
+                T *dst = (T *)(of_v < 0 ? A.k_cache : A.v_cache) + at + (int64_t)h * A.cache_head_stride;
+                dst[ia] = a;
+                if (paired) dst[ib] = b;
+            }
+        }
+    }
+}
+
+template <typename T>
+void launch_pairs(const prep_rotary &R, const prep_rotary_args &A, const RotaryShape &S, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)((A.n_tokens + S.tokens - 1) / S.tokens));
+    if (R.pairing == PREP_PAIR_HALVES)
+        hipLaunchKernelGGL((rotary_pairs<T, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    else
+        hipLaunchKernelGGL((rotary_pairs<T, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+}
+
+// Rows of head_dim elements, n[a] of them stride[a] apart along each of the axes, lie apart from one another.
+bool distinct_rows(int64_t head_dim, const int64_t *stride, const int64_t *n, int axes)
+{
+    int64_t span = head_dim;  // of the axes taken so far
+    bool used[3] = {false, false, false};
+    for (int step = 0; step < axes; step++) {
+        int best = -1;
+        for (int a = 0; a < axes; a++)
+            if (!used[a] && (best < 0 || stride[a] < stride[best])) best = a;
+        used[best] = true;
+        if (n[best] <= 1) continue;
+        if (stride[best] < span) return false;
+        if (stride[best] > (INT64_MAX >> 4) / n[best]) return false;
+        span += stride[best] * (n[best] - 1);
+    }
+    return true;
+}
+
+}  // namespace
+
+}  // namespace prep
+
+using namespace prep;
+
+extern "C" {
+
+int prep_rotary_create(prep_rotary **out, const prep_rotary_config *cfg)
+{
+    if (!out) return PREP_E_INVALID_ARG;
+    *out = nullptr;
+    if (!cfg || cfg->head_dim < 2 || cfg->head_dim > 1024 || !float_type(cfg->dtype) || cfg->reserved != 0 ||
+        (cfg->pairing != PREP_PAIR_HALVES && cfg->pairing != PREP_PAIR_ADJACENT) ||
+        (cfg->order != PREP_SECTIONS_BLOCKS && cfg->order != PREP_SECTIONS_INTERLEAVED) || (cfg->flags & ~(uint32_t)PREP_ROTARY_PER_AXIS) != 0)
+        return PREP_E_INVALID_ARG;
+    int32_t n = 0;
+    for (int a = 0; a < 3; a++) {
+        if (cfg->sections[a] < 0 || cfg->sections[a] > 512) return PREP_E_INVALID_ARG;
+        n += cfg->sections[a];
+    }
+    if (n < 1 || n > cfg->head_dim / 2) return PREP_E_INVALID_ARG;
+    if (!cfg->frequencies && !(cfg->base > 0.0 && std::isfinite(cfg->base))) return PREP_E_INVALID_ARG;
+    uint64_t turns[512];
+    int32_t seen[3] = {0, 0, 0};
+    for (int32_t i = 0; i < n; i++) {
+        int axis;
+        if (cfg->order == PREP_SECTIONS_BLOCKS)
+            axis = i < cfg->sections[0] ? 0 : i < cfg->sections[0] + cfg->sections[1] ? 1 : 2;
+        else
+            axis = i % 3 != 0 && i < 3 * cfg->sections[i % 3] ? i % 3 : 0;
+        long double f;
+        if (cfg->frequencies) {
+            if (!std::isfinite(cfg->frequencies[i])) return PREP_E_INVALID_ARG;
+            f = cfg->frequencies[i];
+        } else if (cfg->flags & PREP_ROTARY_PER_AXIS) {
+            f = cfg->sections[axis] == 0 ? 0.0L : powl((long double)cfg->base, -(long double)seen[axis] / (long double)cfg->sections[axis]);
+        } else {
+            f = powl((long double)cfg->base, -(long double)i / (long double)n);
+        }
+        seen[axis]++;
+        long double t = f / (2.0L * acosl(-1.0L));
+        if (!(t > -1e15L && t < 1e15L)) return PREP_E_INVALID_ARG;
+        t -= floorl(t);
+        // to the nearest multiple of four (two bits are the axis'); a fraction that rounds up to a whole turn is none
+        const long double quarter = floorl(t * 4611686018427387904.0L + 0.5L);
+        const uint64_t q = quarter >= 4611686018427387904.0L ? 0 : (uint64_t)quarter;
+        turns[i] = (q << 2) | (uint64_t)axis;
+    }
+    for (int a = 0; a < 3; a++)
+        if (seen[a] != cfg->sections[a]) return PREP_E_INVALID_ARG;
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || cfg->device < 0 || cfg->device >= ndev) {
+        (void)hipGetLastError();
+        return PREP_E_HIP;
+    }
+    DeviceScope scope(cfg->device);
+    if (!scope.ok()) return PREP_E_HIP;
+    prep_rotary *r = new (std::nothrow) prep_rotary;
+    if (!r) return PREP_E_NOMEM;
+    *r = prep_rotary{cfg->device, cfg->head_dim, n, cfg->dtype, cfg->pairing, nullptr};
+    if (hipMalloc((void **)&r->d_turns, sizeof(uint64_t) * (size_t)n) != hipSuccess ||
+        hipMemcpy(r->d_turns, turns, sizeof(uint64_t) * (size_t)n, hipMemcpyHostToDevice) != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipFree(r->d_turns);
+        delete r;
+        return PREP_E_NOMEM;
+    }
+    *out = r;
+    return PREP_OK;
+}
+
+int prep_rotary_destroy(prep_rotary *r)
+{
+    if (!r) return PREP_E_INVALID_ARG;
+    {
+        DeviceScope scope(r->device);
+        (void)hipDeviceSynchronize();
+        (void)hipFree(r->d_turns);
+        (void)hipGetLastError();
+    }
+    delete r;
+    return PREP_OK;
+}
+
+int prep_rotary_apply(prep_rotary *r, const prep_rotary_args *args, void *stream_ptr)
+{
+    hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
+    if (!r || !args) return PREP_E_INVALID_ARG;
+    prep_rotary_args A = *args;
+    if (A.n_tokens < 0 || A.q_heads < 0 || A.k_heads < 0 || A.q_heads > 65535 || A.k_heads > 65535 || A.q_heads + A.k_heads == 0 ||
+        A.axis_stride < 0 || (A.inverse != 0 && A.inverse != 1))
+        return PREP_E_INVALID_ARG;
+    const bool store = A.k_cache != nullptr;
+    if (store != (A.v_cache != nullptr)) return PREP_E_INVALID_ARG;
+    if (A.n_tokens == 0) return PREP_OK;
+    const uintptr_t size = (uintptr_t)element_bytes(r->dtype);
+    auto input = [&](const prep_heads &x) { return x.data && aligned(x.data, size) && x.token_stride >= 0 && x.head_stride >= 0; };
+    auto output = [&](const prep_heads &x, const prep_heads &from, int64_t heads) {
+        const int64_t stride[2] = {x.token_stride, x.head_stride}, n[2] = {A.n_tokens, heads};
+        if (!input(x) || !distinct_rows(r->head_dim, stride, n, 2)) return false;
+        // in place: every value goes back where it came from
+        return x.data != from.data || ((A.n_tokens == 1 || x.token_stride == from.token_stride) && (heads == 1 || x.head_stride == from.head_stride));
+    };
+    if (!A.positions || !aligned(A.positions, 4)) return PREP_E_INVALID_ARG;
+    if (A.q_heads > 0 && (!input(A.q) || !output(A.q_out, A.q, A.q_heads))) return PREP_E_INVALID_ARG;
+    if (A.k_heads > 0) {
+        if (!input(A.k)) return PREP_E_INVALID_ARG;
+        if (!(store && !A.k_out.data) && !output(A.k_out, A.k, A.k_heads)) return PREP_E_INVALID_ARG;
+    }
+    if (store) {
+        if (A.k_heads == 0 || !input(A.v) || !A.slots || !aligned(A.slots, 8) || A.block_size < 1 || A.n_blocks < 0 || A.n_blocks > 0x7FFFFFFF ||
+            A.k_cache == A.v_cache || !aligned(A.k_cache, size) || !aligned(A.v_cache, size))
+            return PREP_E_INVALID_ARG;
+        const int64_t stride[3] = {A.block_stride, A.slot_stride, A.cache_head_stride}, n[3] = {A.n_blocks, A.block_size, A.k_heads};
+        for (int64_t s : stride)
+            if (s < 0) return PREP_E_INVALID_ARG;
+        if (!distinct_rows(r->head_dim, stride, n, 3)) return PREP_E_INVALID_ARG;
+    }
+    DeviceScope scope(r->device);
+    if (!scope.ok()) return PREP_E_HIP;
+    RotaryShape S;
+    S.head_dim = r->head_dim;
+    S.pairs = r->pairs;
+    S.tokens = kTrig / r->pairs < kMaxTokens ? kTrig / r->pairs : kMaxTokens;
+    if ((A.n_tokens + S.tokens - 1) / S.tokens > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
+    if (r->dtype == PREP_F32) launch_pairs<float>(*r, A, S, stream);
+    else if (r->dtype == PREP_F16) launch_pairs<__half>(*r, A, S, stream);
+    else launch_pairs<__hip_bfloat16>(*r, A, S, stream);
+    return hipGetLastError() == hipSuccess ? PREP_OK : PREP_E_HIP;
+}
+
+}  // extern "C"
