@@ -55,7 +55,8 @@ __device__ __forceinline__ int64_t cache_row(const prep_rotary_args &A, int64_t 
 {
     const int64_t slot = A.slots[i];
     if (slot < 0 || slot >= A.n_blocks * A.block_size) return -1;
-    const int64_t block = slot / A.block_size;
+    // (a 64-bit division takes some 100 instructions, and hardly any cache has 2^32 slots)
+    const int64_t block = slot <= 0xFFFFFFFF ? (int64_t)((uint32_t)slot / (uint32_t)A.block_size) : slot / A.block_size;
     return block * A.block_stride + (slot - block * A.block_size) * A.slot_stride;
 }
 
@@ -114,14 +115,199 @@ __global__ __launch_bounds__(kThreads) void rotary_pairs(prep_rotary_args A, Rot
     }
 }
 
+// Aligned rows.  A lane takes 32 bytes of a head's row in two loads of 16 (kHalves: values i.. and i + n.., whose pairs meet in
+// the lane), always the same places of a row, and kRows rows one after the other whose loads go out together, before the
+// angles are formed.  A token's angles are formed once per workgroup and shared by all its heads.
+struct RowShape {
+    int32_t units;           // lanes of a row
+    int32_t step;            // rows that a workgroup holds at a time
+    int32_t heads;           // of q, k and (with a cache) v
+    int32_t tokens;          // most of a workgroup
+    int32_t head_dim, pairs;
+    int64_t rows;            // of the call
+};
+
+// Angles and tokens of a workgroup: 18 KB of LDS, which leaves a compute unit its eight workgroups.
+constexpr int kMostAngles = 2048, kMostTokens = 256;
+
 template <typename T>
-void launch_pairs(const prep_rotary &R, const prep_rotary_args &A, const RotaryShape &S, hipStream_t stream)
+union Vec {
+    uint4 raw;
+    T v[16 / sizeof(T)];
+};
+
+template <typename T, bool kHalves, int kRows>
+__global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowShape S, const uint64_t *__restrict__ turns)
 {
-    const dim3 grid((uint32_t)((A.n_tokens + S.tokens - 1) / S.tokens));
-    if (R.pairing == PREP_PAIR_HALVES)
+    constexpr int kV = 16 / (int)sizeof(T);
+    __shared__ alignas(16) float cosine[kMostAngles], sine[kMostAngles];
+    __shared__ int64_t place_in_cache[kMostTokens];
+
+    const int64_t row0 = (int64_t)blockIdx.x * (S.step * kRows);
+    const int64_t token0 = S.rows <= 0xFFFFFFFF ? (int64_t)((uint32_t)row0 / (uint32_t)S.heads) : row0 / S.heads;
+    const int head0 = (int)(row0 - token0 * S.heads);
+    const int lane_row = (int)threadIdx.x / S.units, u = (int)threadIdx.x - lane_row * S.units;
+    const bool works = lane_row < S.step;
+    // the lane's places in a row
+    const int rotated = 2 * S.pairs, rotary_units = S.pairs / kV;
+    int at_a, at_b;
+    if (kHalves) {
+        const int tail = u - rotary_units;
+        at_a = tail < 0 ? u * kV : rotated + 2 * tail * kV;
+        at_b = tail < 0 ? u * kV + S.pairs : at_a + kV;
+    } else {
+        at_a = u * kV;
+        at_b = (u + S.units) * kV;
+    }
+    const bool has_b = at_b < S.head_dim;
+    const bool store = A.k_cache != nullptr;
+
+    Vec<T> a[kRows], b[kRows];
+    int token[kRows], head[kRows];  // of the rows; token -1: none
+    {
+        int t = 0, h = head0 + lane_row;
+#pragma unroll
+        for (int k = 0; k < kRows; k++) {
+            while (h >= S.heads) {
+                h -= S.heads;
+                t++;
+            }
+            const bool mine = works && row0 + lane_row + k * S.step < S.rows;
+            token[k] = mine ? t : -1;
+            head[k] = h;
+            if (mine) {
+                const int of_k = h - A.q_heads, of_v = of_k - A.k_heads;
+                const T *base = (const T *)(of_k < 0 ? A.q.data : of_v < 0 ? A.k.data : A.v.data);
+                const int64_t ts = of_k < 0 ? A.q.token_stride : of_v < 0 ? A.k.token_stride : A.v.token_stride;
+                const int64_t hs = of_k < 0 ? A.q.head_stride : of_v < 0 ? A.k.head_stride : A.v.head_stride;
+                const T *src = base + (token0 + t) * ts + (of_k < 0 ? h : of_v < 0 ? of_k : of_v) * hs;
+                a[k].raw = *reinterpret_cast<const uint4 *>(src + at_a);
+                if (has_b) b[k].raw = *reinterpret_cast<const uint4 *>(src + at_b);
+            }
+            h += S.step;
+        }
+    }
+    const int n = (int)min((int64_t)S.tokens, A.n_tokens - token0);
+    for (int e = threadIdx.x; e < n * S.pairs; e += kThreads) {
+        const int t = e / S.pairs, p = e - t * S.pairs;
+        const uint64_t f = turns[p];
+        const int64_t place = A.positions[(int64_t)(f & 3u) * A.axis_stride + token0 + t];
+        const float2 cs = cos_sin((uint64_t)place * (f & ~(uint64_t)3));
+        cosine[e] = cs.x;
+        sine[e] = A.inverse ? -cs.y : cs.y;
+    }
+    if (store)
+        for (int t = threadIdx.x; t < n; t += kThreads) place_in_cache[t] = cache_row(A, token0 + t);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kRows; k++) {
+        if (token[k] < 0) continue;
+        const int h = head[k], of_k = h - A.q_heads, of_v = of_k - A.k_heads;
+        if (of_v < 0) {
+            const float *c = cosine + token[k] * S.pairs, *s = sine + token[k] * S.pairs;
+            if (kHalves) {
+                if (u < rotary_units) {
+#pragma unroll
+                    for (int j = 0; j < kV; j++) {
+                        const float x = to_float(a[k].v[j]), y = to_float(b[k].v[j]), cj = c[at_a + j], sj = s[at_a + j];
+                        a[k].v[j] = from_float<T>(fmaf(x, cj, -y * sj));
+                        b[k].v[j] = from_float<T>(fmaf(x, sj, y * cj));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    Vec<T> &w = half == 0 ? a[k] : b[k];
+                    const int at = half == 0 ? at_a : at_b;
+                    if (at < rotated) {
+#pragma unroll
+                        for (int j = 0; j < kV / 2; j++) {
+                            const float x = to_float(w.v[2 * j]), y = to_float(w.v[2 * j + 1]), cj = c[at / 2 + j], sj = s[at / 2 + j];
+                            w.v[2 * j] = from_float<T>(fmaf(x, cj, -y * sj));
+                            w.v[2 * j + 1] = from_float<T>(fmaf(x, sj, y * cj));
+                        }
+                    }
+                }
+            }
+            T *out = (T *)(of_k < 0 ? A.q_out.data : A.k_out.data);
+            if (out != nullptr) {
+                out += (token0 + token[k]) * (of_k < 0 ? A.q_out.token_stride : A.k_out.token_stride) +
+                       (of_k < 0 ? h * A.q_out.head_stride : of_k * A.k_out.head_stride);
+                *reinterpret_cast<uint4 *>(out + at_a) = a[k].raw;
+                if (has_b) *reinterpret_cast<uint4 *>(out + at_b) = b[k].raw;
+            }
+        }
+        if (store && of_k >= 0) {
+            const int64_t at = place_in_cache[token[k]];
+            if (at >= 0) {
+                T *out = (T *)(of_v < 0 ? A.k_cache : A.v_cache) + at + (of_v < 0 ? of_k : of_v) * A.cache_head_stride;
+                *reinterpret_cast<uint4 *>(out + at_a) = a[k].raw;
+                if (has_b) *reinterpret_cast<uint4 *>(out + at_b) = b[k].raw;
+            }
+        }
+    }
+}
+
+// Whether all rows of a call can be read and written 16 bytes at a time, pairs whole.
+bool rows_aligned(const prep_rotary &R, const prep_rotary_args &A)
+{
+    const int64_t v = 16 / element_bytes(R.dtype);
+    if (R.head_dim % v != 0 || (R.pairing == PREP_PAIR_HALVES ? R.pairs : 2 * R.pairs) % v != 0) return false;
+    auto fits = [&](const void *p, int64_t s, int64_t t) { return aligned(p, 16) && s % v == 0 && t % v == 0; };
+    auto rows = [&](const prep_heads &x) { return x.data == nullptr || fits(x.data, x.token_stride, x.head_stride); };
+    if (A.q_heads > 0 && !(rows(A.q) && rows(A.q_out))) return false;
+    if (A.k_heads > 0 && !(rows(A.k) && rows(A.k_out))) return false;
+    if (A.k_cache != nullptr)
+        return rows(A.v) && fits(A.k_cache, A.block_stride, A.slot_stride) && fits(A.v_cache, A.cache_head_stride, 0);
+    return true;
+}
+
+constexpr int kManyRows = 4;  // rows of a lane in large calls
+
+template <typename T, bool kHalves>
+int launch_rows(const prep_rotary &R, const prep_rotary_args &A, hipStream_t stream)
+{
+    const int v = 16 / (int)sizeof(T);
+    RowShape S;
+    S.head_dim = R.head_dim;
+    S.pairs = R.pairs;
+    S.units = kHalves ? R.pairs / v + ((R.head_dim - 2 * R.pairs) / v + 1) / 2 : (R.head_dim / v + 1) / 2;
+    S.heads = A.q_heads + A.k_heads * (A.k_cache != nullptr ? 2 : 1);
+    S.rows = A.n_tokens * S.heads;
+    S.step = kThreads / S.units;
+    auto tokens_of = [&](int rows) { return (rows + S.heads - 2) / S.heads + 1; };
+    int per_lane = S.rows >= (int64_t)S.step * kManyRows * 512 ? kManyRows : 1;
+    auto fit = [&](int rows) { return tokens_of(rows) <= kMostTokens && tokens_of(rows) * S.pairs <= kMostAngles; };
+    if (!fit(S.step * per_lane)) per_lane = 1;
+    while (S.step > 1 && !fit(S.step)) S.step--;  // (one row is of one token, and a head has at most 512 pairs)
+    S.tokens = tokens_of(S.step * per_lane);
+    const int64_t blocks = (S.rows + S.step * per_lane - 1) / (S.step * per_lane);
+    if (blocks > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
+    const dim3 grid((uint32_t)blocks);
+    if (per_lane == 1)
+        hipLaunchKernelGGL((rotary_rows<T, kHalves, 1>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    else
+        hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    return PREP_OK;
+}
+
+template <typename T>
+int launch_for(const prep_rotary &R, const prep_rotary_args &A, hipStream_t stream)
+{
+    const bool halves = R.pairing == PREP_PAIR_HALVES;
+    if (rows_aligned(R, A)) return halves ? launch_rows<T, true>(R, A, stream) : launch_rows<T, false>(R, A, stream);
+    RotaryShape S;
+    S.head_dim = R.head_dim;
+    S.pairs = R.pairs;
+    S.tokens = kTrig / R.pairs < kMaxTokens ? kTrig / R.pairs : kMaxTokens;
+    const int64_t blocks = (A.n_tokens + S.tokens - 1) / S.tokens;
+    if (blocks > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
+    const dim3 grid((uint32_t)blocks);
+    if (halves)
         hipLaunchKernelGGL((rotary_pairs<T, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
     else
         hipLaunchKernelGGL((rotary_pairs<T, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    return PREP_OK;
 }
 
 // Rows of head_dim elements, n[a] of them stride[a] apart along each of the axes, lie apart from one another.
@@ -263,14 +449,10 @@ int prep_rotary_apply(prep_rotary *r, const prep_rotary_args *args, void *stream
     }
     DeviceScope scope(r->device);
     if (!scope.ok()) return PREP_E_HIP;
-    RotaryShape S;
-    S.head_dim = r->head_dim;
-    S.pairs = r->pairs;
-    S.tokens = kTrig / r->pairs < kMaxTokens ? kTrig / r->pairs : kMaxTokens;
-    if ((A.n_tokens + S.tokens - 1) / S.tokens > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
-    if (r->dtype == PREP_F32) launch_pairs<float>(*r, A, S, stream);
-    else if (r->dtype == PREP_F16) launch_pairs<__half>(*r, A, S, stream);
-    else launch_pairs<__hip_bfloat16>(*r, A, S, stream);
+    const int rc = r->dtype == PREP_F32   ? launch_for<float>(*r, A, stream)
+                   : r->dtype == PREP_F16 ? launch_for<__half>(*r, A, stream)
+                                          : launch_for<__hip_bfloat16>(*r, A, stream);
+    if (rc != PREP_OK) return rc;
     return hipGetLastError() == hipSuccess ? PREP_OK : PREP_E_HIP;
 }
 
