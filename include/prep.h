@@ -542,6 +542,7 @@ int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n
  *   free_left      DEVICE, one entry, another than free_count: blocks left on the stack.  A caller that keeps
  *                  the stack passes it as the next call's free_count.
  *   workspace      as above, prep_block_slots_workspace(n) bytes
+ * What is written must not overlap what is read.
  */
 typedef struct {
     int32_t n;                 /* requests, 0..1048576                              */

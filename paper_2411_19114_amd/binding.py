@@ -1,6 +1,7 @@
 """ctypes marshalling for libprep.so.  Same names as the C ABI, no arithmetic."""
 import ctypes as C
 import os
+import struct
 import subprocess
 
 import numpy as np
@@ -71,29 +72,16 @@ class PatchParams(C.Structure):
                 ("min_pixels", C.c_int64), ("max_pixels", C.c_int64)]
 
 
-class BlockArgs(C.Structure):
-    _fields_ = [("n", C.c_int32), ("block_size", C.c_int32), ("n_blocks", C.c_int64), ("cached", C.c_void_p), ("fresh", C.c_void_p),
-                ("free_blocks", C.c_void_p), ("free_capacity", C.c_int32), ("table_width", C.c_int32), ("free_count", C.c_void_p),
-                ("table", C.c_void_p), ("table_stride", C.c_int64), ("capacity", C.c_int64), ("slots", C.c_void_p),
-                ("token_starts", C.c_void_p), ("lengths", C.c_void_p), ("status", C.c_void_p), ("free_left", C.c_void_p),
-                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
-
-
 class RotaryConfig(C.Structure):
     _fields_ = [("device", C.c_int32), ("head_dim", C.c_int32), ("sections", C.c_int32 * 3), ("dtype", C.c_int32),
                 ("pairing", C.c_int32), ("order", C.c_int32), ("flags", C.c_uint32), ("reserved", C.c_int32), ("base", C.c_double),
                 ("frequencies", C.POINTER(C.c_double))]
 
 
-class Heads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
-
-
-class RotaryArgs(C.Structure):
-    _fields_ = [("n_tokens", C.c_int64), ("positions", C.c_void_p), ("axis_stride", C.c_int64), ("q", Heads), ("q_out", Heads),
-                ("k", Heads), ("k_out", Heads), ("v", Heads), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("inverse", C.c_int32),
-                ("block_size", C.c_int32), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("n_blocks", C.c_int64),
-                ("block_stride", C.c_int64), ("slot_stride", C.c_int64), ("cache_head_stride", C.c_int64), ("slots", C.c_void_p)]
+# prep_block_args and prep_rotary_args (five prep_heads behind the first three members): packed at every call, in a
+# quarter of the time that filling a ctypes structure takes
+_BLOCK_ARGS = struct.Struct("iiqQQQiiQQqqQQQQQQQ")
+_ROTARY_ARGS = struct.Struct("qQq" + "Qqq" * 5 + "iiiiQQqqqqQ")
 
 
 class ServerConfig(C.Structure):
@@ -201,8 +189,8 @@ def lib():
         L.prep_audio_features.argtypes = [vp, vp, u64p, C.c_int32, C.c_int32, vp, u64p, vp]
         i64p = C.POINTER(C.c_int64)
         L.prep_patch_grid.argtypes = [C.POINTER(PatchParams), C.c_int32, C.c_int32, C.c_int32, i32p]
-        L.prep_patch_rows.argtypes = [C.c_int32, vp, u64p, i32p, i32p, i32p, i32p, u64p, C.c_int32, C.POINTER(PatchParams), vp,
-                                      C.c_int64, C.c_int64, i64p, vp]
+        L.prep_patch_rows.argtypes = [C.c_int32, vp, vp, vp, vp, vp, vp, vp, C.c_int32, C.POINTER(PatchParams), vp, C.c_int64, C.c_int64,
+                                      i64p, vp]
         L.prep_decode_patches_batch.argtypes = [vp, u8p, vp, u64p, C.c_int32, C.POINTER(PatchParams), vp, C.c_int64, C.c_int64, i64p, vp]
         L.prep_token_positions_workspace.argtypes = [C.c_int32]
         L.prep_token_positions_workspace.restype = C.c_uint64
@@ -210,10 +198,10 @@ def lib():
                                            C.c_uint64, vp]
         L.prep_block_slots_workspace.argtypes = [C.c_int32]
         L.prep_block_slots_workspace.restype = C.c_uint64
-        L.prep_block_slots.argtypes = [C.c_int32, C.POINTER(BlockArgs), vp]
+        L.prep_block_slots.argtypes = [C.c_int32, vp, vp]
         L.prep_rotary_create.argtypes = [C.POINTER(vp), C.POINTER(RotaryConfig)]
         L.prep_rotary_destroy.argtypes = [vp]
-        L.prep_rotary_apply.argtypes = [vp, C.POINTER(RotaryArgs), vp]
+        L.prep_rotary_apply.argtypes = [vp, vp, vp]
         _lib = L
     return _lib
 
@@ -506,9 +494,10 @@ class AudioPreprocessor:
 # ---- batches for language models that read images and video ----------------------------------------
 
 
-def _list(kind, values):
+def _packed(kind, values):
+    """Host numbers as the C array that a call reads ("Q" = uint64_t, "i" = int32_t)."""
     values = values.tolist() if isinstance(values, np.ndarray) else values
-    return (kind * len(values))(*values)
+    return struct.pack(f"{len(values)}{kind}", *values)
 
 
 def make_patch_params(patch, merge, frames_per_patch, out_dtype, mean, std, filter=FILTER_BILINEAR, min_pixels=0, max_pixels=0):
@@ -534,9 +523,9 @@ def patch_rows(device, rgb_ptr, rgb_offsets, widths, heights, pitches, params, o
     n = len(widths)
     starts = (C.c_int64 * (n + 1))()
     _check(lib().prep_patch_rows(
-        device, rgb_ptr, _list(C.c_uint64, rgb_offsets), _list(C.c_int32, widths), _list(C.c_int32, heights), _list(C.c_int32, pitches),
-        None if frames is None else _list(C.c_int32, frames), None if frame_strides is None else _list(C.c_uint64, frame_strides), n,
-        C.byref(params), out_ptr, out_stride, out_rows, starts, stream), "prep_patch_rows")
+        device, rgb_ptr, _packed("Q", rgb_offsets), _packed("i", widths), _packed("i", heights), _packed("i", pitches),
+        None if frames is None else _packed("i", frames), None if frame_strides is None else _packed("Q", frame_strides), n,
+        params, out_ptr, out_stride, out_rows, starts, stream), "prep_patch_rows")
     return list(starts)
 
 
@@ -559,9 +548,9 @@ def block_slots(n, block_size, n_blocks, cached_ptr, fresh_ptr, free_blocks_ptr,
                 table_width, slots_ptr, capacity, token_starts_ptr, lengths_ptr, status_ptr, free_left_ptr, workspace_ptr, workspace_bytes,
                 device=0, stream=0):
     """prep_block_slots: block tables and slot map of a batch's new tokens, from device arrays."""
-    args = BlockArgs(n, block_size, n_blocks, cached_ptr, fresh_ptr, free_blocks_ptr, free_capacity, table_width, free_count_ptr, table_ptr,
-                     table_stride, capacity, slots_ptr, token_starts_ptr, lengths_ptr, status_ptr, free_left_ptr, workspace_ptr, workspace_bytes)
-    _check(lib().prep_block_slots(device, C.byref(args), stream), "prep_block_slots")
+    _check(lib().prep_block_slots(device, _BLOCK_ARGS.pack(
+        n, block_size, n_blocks, cached_ptr, fresh_ptr, free_blocks_ptr, free_capacity, table_width, free_count_ptr, table_ptr, table_stride,
+        capacity, slots_ptr, token_starts_ptr, lengths_ptr, status_ptr, free_left_ptr, workspace_ptr, workspace_bytes), stream), "prep_block_slots")
 
 
 class Rotary:
@@ -571,7 +560,7 @@ class Rotary:
         cfg = RotaryConfig(device, head_dim, (C.c_int32 * 3)(*sections), {"f32": F32, "f16": F16, "bf16": BF16}.get(dtype, dtype), pairing, order,
                            ROTARY_PER_AXIS if per_axis else 0, 0, float(base or 0.0), None)
         if frequencies is not None:
-            cfg.frequencies = _list(C.c_double, [float(f) for f in frequencies])
+            cfg.frequencies = (C.c_double * len(frequencies))(*[float(f) for f in frequencies])
             if len(frequencies) != sum(sections):
                 raise PrepError(E_INVALID_ARG, "prep_rotary_create")
         self._h = C.c_void_p()
@@ -580,9 +569,9 @@ class Rotary:
     def apply(self, n_tokens, positions, axis_stride, q=(0, 0, 0), q_out=(0, 0, 0), q_heads=0, k=(0, 0, 0), k_out=(0, 0, 0), k_heads=0,
               v=(0, 0, 0), inverse=False, k_cache=0, v_cache=0, n_blocks=0, block_size=0, block_stride=0, slot_stride=0, cache_head_stride=0,
               slots=0, stream=0):
-        args = RotaryArgs(n_tokens, positions, axis_stride, q, q_out, k, k_out, v, q_heads, k_heads, 1 if inverse else 0, block_size, k_cache,
-                          v_cache, n_blocks, block_stride, slot_stride, cache_head_stride, slots)
-        _check(lib().prep_rotary_apply(self._h, C.byref(args), stream), "prep_rotary_apply")
+        _check(lib().prep_rotary_apply(self._h, _ROTARY_ARGS.pack(
+            n_tokens, positions, axis_stride, *q, *q_out, *k, *k_out, *v, q_heads, k_heads, 1 if inverse else 0, block_size, k_cache, v_cache,
+            n_blocks, block_stride, slot_stride, cache_head_stride, slots), stream), "prep_rotary_apply")
 
     def close(self):
         if self._h:

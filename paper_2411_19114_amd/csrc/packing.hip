@@ -1,6 +1,10 @@
 // Places and cache slots of the tokens of a packed batch (gfx950): whole-number work on lists of
 // lengths that lie on the GPU.  Both operators are a prefix sum over the list (segments of
 // sequences, or requests) and then a search in it for every token.
+//
+// Up to kListed entries one launch does both: every workgroup sums the whole list in LDS, which costs it a few
+// microseconds beside the others, and places a share of the tokens.  Longer lists are summed by one workgroup into
+// the workspace, and a second launch searches there.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -15,27 +19,38 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kScanThreads = 1024, kWaves = kScanThreads / 64;
 constexpr int32_t kMaxEntries = 1 << 20;
+// One launch: a workgroup's threads, the longest list, entries and tokens of a thread.
+constexpr int kListThreads = 512, kListWaves = kListThreads / 64, kListed = 4096, kPerThread = kListed / kListThreads;
+constexpr int kTokensPerThread = 4, kTokensPerWg = kListThreads * kTokensPerThread;
 
-// Inclusive sums of v over the lanes up to one's own, in a workgroup of kScanThreads; *total = over all.
-template <typename T>
-__device__ T scan_block(T v, T *total)
+struct Sum {
+    template <typename T> __device__ T operator()(T a, T b) const { return a + b; }
+};
+struct Largest {
+    template <typename T> __device__ T operator()(T a, T b) const { return a < b ? b : a; }
+};
+// v of the lanes before one's own taken together, in a workgroup of kScanWaves waves; *total = of all.  0 is the
+// operation's neutral value.
+template <int kScanWaves, typename T, typename Op>
+__device__ T scan_block(T v, T *total, Op op)
 {
-    __shared__ T wave_sum[kWaves];
+    __shared__ T wave_sum[kScanWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int d = 1; d < 64; d *= 2) {
         const T u = __shfl_up(v, (unsigned)d);
-        if (lane >= d) v += u;
+        if (lane >= d) v = op(u, v);
     }
+    const T left = __shfl_up(v, 1u);
     if (lane == 63) wave_sum[wave] = v;
     __syncthreads();
     T before = 0, all = 0;
-    for (int w = 0; w < kWaves; w++) {
-        if (w < wave) before += wave_sum[w];
-        all += wave_sum[w];
+    for (int w = 0; w < kScanWaves; w++) {
+        if (w < wave) before = op(before, wave_sum[w]);
+        all = op(all, wave_sum[w]);
     }
     __syncthreads();
     *total = all;
-    return v + before;
+    return lane == 0 ? before : op(before, left);
 }
 
 __device__ __forceinline__ int32_t clip31(uint64_t v) { return v > 0x7FFFFFFFull ? 0x7FFFFFFF : (int32_t)v; }
@@ -88,11 +103,11 @@ __global__ __launch_bounds__(kScanThreads) void sum_segments(SegmentList L, int3
         uint64_t tokens = 0, tokens_all;
         uint32_t advance = 0, moved_all;
         if (j >= lo && j < hi) segment_size(L.segments[j], &tokens, &advance);
-        const uint64_t tokens_to = scan_block<uint64_t>(tokens, &tokens_all);
-        const uint32_t moved_to = scan_block<uint32_t>(advance, &moved_all);
+        const uint64_t token = scan_block<kWaves, uint64_t>(tokens, &tokens_all, Sum());
+        const uint32_t move = scan_block<kWaves, uint32_t>(advance, &moved_all, Sum());
         if (j < L.n_segments) {
-            starts[j] = clip31(tokens_before + tokens_to - tokens);
-            moved[j] = moved_before + moved_to - advance;
+            starts[j] = clip31(tokens_before + token);
+            moved[j] = moved_before + move;
         }
         tokens_before += tokens_all;
         moved_before += moved_all;
@@ -101,6 +116,36 @@ __global__ __launch_bounds__(kScanThreads) void sum_segments(SegmentList L, int3
         starts[L.n_segments] = clip31(tokens_before);
         moved[L.n_segments] = moved_before;
     }
+}
+
+// Place of token r of a segment that starts at place `base`.
+struct Place {
+    uint32_t t, h, w;
+};
+__device__ __forceinline__ Place place_in_segment(const prep_segment &s, uint32_t base, uint32_t r, int32_t merge)
+{
+    Place p;
+    p.t = p.h = p.w = base + r;
+    if (s.h != 0) {
+        const uint32_t h = (uint32_t)s.h, w = (uint32_t)s.w, m = (uint32_t)merge;
+        const uint32_t a = r / (h * w), r1 = r - a * (h * w);
+        p.t = base + a * (uint32_t)s.step;
+        if (merge == 1) {
+            const uint32_t y = r1 / w;
+            p.h = base + y;
+            p.w = base + (r1 - y * w);
+        } else {
+            // bands of m rows, windows of m columns in a band, both shorter at the edge
+            const uint32_t band = r1 / (m * w), r2 = r1 - band * (m * w);
+            const uint32_t tall = min(m, h - band * m);
+            const uint32_t window = r2 / (tall * m), r3 = r2 - window * (tall * m);
+            const uint32_t wide = min(m, w - window * m);
+            const uint32_t y = r3 / wide;
+            p.h = base + band * m + y;
+            p.w = base + window * m + (r3 - y * wide);
+        }
+    }
+    return p;
 }
 
 __global__ __launch_bounds__(kThreads) void place_tokens(SegmentList L, int32_t merge, const int32_t *__restrict__ starts,
@@ -115,32 +160,107 @@ __global__ __launch_bounds__(kThreads) void place_tokens(SegmentList L, int32_t 
             next[i] = (int32_t)((L.first ? (uint32_t)L.first[i] : 0u) + moved[seq_bound(L, (int)i + 1)] - moved[b]);
     }
     if (i >= capacity) return;
-    uint32_t pt = 0, ph = 0, pw = 0;
+    Place p = {0, 0, 0};
     if (i < starts[L.n_segments]) {
         const int j = last_not_above(starts, L.n_segments, i);
         const int q = last_not_above(L.seq_segments, L.n_seq, j);
-        const prep_segment s = L.segments[j];
         const uint32_t base = (L.first ? (uint32_t)L.first[q] : 0u) + moved[j] - moved[seq_bound(L, q)];
-        const uint32_t r = (uint32_t)i - (uint32_t)starts[j];
-        if (s.h == 0) {
-            pt = ph = pw = base + r;
-        } else {
-            const uint32_t h = (uint32_t)s.h, w = (uint32_t)s.w, m = (uint32_t)merge;
-            const uint32_t a = r / (h * w), r1 = r - a * (h * w);
-            // bands of m rows, windows of m columns in a band, both shorter at the edge
-            const uint32_t band = r1 / (m * w), r2 = r1 - band * (m * w);
-            const uint32_t tall = min(m, h - band * m);
-            const uint32_t window = r2 / (tall * m), r3 = r2 - window * (tall * m);
-            const uint32_t wide = min(m, w - window * m);
-            const uint32_t y = r3 / wide;
-            pt = base + a * (uint32_t)s.step;
-            ph = base + band * m + y;
-            pw = base + window * m + (r3 - y * wide);
+        p = place_in_segment(L.segments[j], base, (uint32_t)i - (uint32_t)starts[j], merge);
+    }
+    positions[i] = (int32_t)p.t;
+    positions[capacity + i] = (int32_t)p.h;
+    positions[2 * capacity + i] = (int32_t)p.w;
+}
+
+// The same in one launch, for lists of at most kListed segments and as many sequences.
+__global__ __launch_bounds__(kListThreads) void place_listed(SegmentList L, int32_t merge, int32_t *__restrict__ positions,
+                                                             int64_t capacity, int32_t *__restrict__ token_starts,
+                                                             int32_t *__restrict__ next)
+{
+    // first tokens of the segments; how far places have moved before each; and first the sequence that begins at a
+    // segment (+ 1, 0 = none), then the place where the segment starts
+    __shared__ alignas(16) int32_t starts[kListed + kPerThread];
+    __shared__ alignas(16) uint32_t moved[kListed + kPerThread], base[kListed + kPerThread];
+    const int32_t n = L.n_segments, lo = seq_bound(L, 0), hi = seq_bound(L, L.n_seq);
+    for (int32_t j = threadIdx.x; j <= n; j += kListThreads) base[j] = 0;
+    __syncthreads();
+    for (int32_t q = threadIdx.x; q < L.n_seq; q += kListThreads) atomicMax(&base[seq_bound(L, q)], (uint32_t)q + 1);
+    for (int32_t j = threadIdx.x; j < n; j += kListThreads) {
+        uint64_t tokens = 0;
+        uint32_t advance = 0;
+        if (j >= lo && j < hi) segment_size(L.segments[j], &tokens, &advance);
+        starts[j] = clip31(tokens);
+        moved[j] = advance;
+    }
+    __syncthreads();
+    const int32_t j0 = (int32_t)threadIdx.x * kPerThread;
+    uint64_t tokens = 0, tokens_all;
+    uint32_t advance = 0, moved_all, sequence = 0, sequences;
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++) {
+        if (j0 + k < n) {
+            tokens += (uint64_t)(uint32_t)starts[j0 + k];
+            advance += moved[j0 + k];
+            if (base[j0 + k] > sequence) sequence = base[j0 + k];
         }
     }
-    positions[i] = (int32_t)pt;
-    positions[capacity + i] = (int32_t)ph;
-    positions[2 * capacity + i] = (int32_t)pw;
+    uint64_t token = scan_block<kListWaves, uint64_t>(tokens, &tokens_all, Sum());
+    uint32_t move = scan_block<kListWaves, uint32_t>(advance, &moved_all, Sum());
+    uint32_t q = scan_block<kListWaves, uint32_t>(sequence, &sequences, Largest());  // the sequence of the segment before
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++) {
+        if (j0 + k < n) {
+            const uint64_t mine = (uint64_t)(uint32_t)starts[j0 + k];
+            const uint32_t far = moved[j0 + k];
+            starts[j0 + k] = clip31(token);
+            moved[j0 + k] = move;
+            token += mine;
+            move += far;
+        }
+    }
+    if (threadIdx.x == 0) {
+        starts[n] = clip31(tokens_all);
+        moved[n] = moved_all;
+    }
+    __syncthreads();
+    {
+        uint32_t from = 0;
+        bool known = false;
+#pragma unroll
+        for (int k = 0; k < kPerThread; k++) {
+            if (j0 + k < n) {
+                if (base[j0 + k] != 0) {
+                    q = base[j0 + k];
+                    known = false;
+                }
+                if (!known && q != 0) {
+                    from = (L.first ? (uint32_t)L.first[q - 1] : 0u) - moved[seq_bound(L, (int)q - 1)];
+                    known = true;
+                }
+                base[j0 + k] = from + moved[j0 + k];
+            }
+        }
+    }
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int32_t q = threadIdx.x; q <= L.n_seq; q += kListThreads) {
+            const int32_t b = seq_bound(L, q);
+            token_starts[q] = starts[b];
+            if (next != nullptr && q < L.n_seq) next[q] = (int32_t)((L.first ? (uint32_t)L.first[q] : 0u) + moved[seq_bound(L, q + 1)] - moved[b]);
+        }
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; k++) {
+        const int64_t i = (int64_t)blockIdx.x * kTokensPerWg + k * kListThreads + threadIdx.x;
+        if (i >= capacity) break;
+        Place p = {0, 0, 0};
+        if (i < starts[n]) {
+            const int j = last_not_above(starts, n, i);
+            p = place_in_segment(L.segments[j], base[j], (uint32_t)i - (uint32_t)starts[j], merge);
+        }
+        positions[i] = (int32_t)p.t;
+        positions[capacity + i] = (int32_t)p.h;
+        positions[2 * capacity + i] = (int32_t)p.w;
+    }
 }
 
 // ---- slots ---------------------------------------------------------------------------------------
@@ -170,12 +290,12 @@ __global__ __launch_bounds__(kScanThreads) void sum_requests(prep_block_args A, 
             if (!sound) cached = fresh = 0;
         }
         uint64_t tokens_all, needed_all;
-        const uint64_t tokens_to = tokens_before + scan_block<uint64_t>((uint64_t)fresh, &tokens_all);
+        const uint64_t tokens_to = tokens_before + scan_block<kWaves, uint64_t>((uint64_t)fresh, &tokens_all, Sum()) + (uint64_t)fresh;
         const uint32_t after = (uint32_t)cached + (uint32_t)fresh;
         const uint32_t had = blocks_of((uint32_t)cached, (uint32_t)A.block_size), want = blocks_of(after, (uint32_t)A.block_size);
         const bool fits = sound && after <= (uint32_t)INT32_MAX && want <= (uint32_t)A.table_width && tokens_to <= (uint64_t)A.capacity;
         const uint32_t need = fits ? want - had : 0;
-        const uint64_t needed_to = needed_before + scan_block<uint64_t>(need, &needed_all);
+        const uint64_t needed_to = needed_before + scan_block<kWaves, uint64_t>(need, &needed_all, Sum()) + need;
         const bool granted = fits && (need == 0 || needed_to <= (uint64_t)on_stack);
         if (granted && need != 0) atomicMax(&used, (uint32_t)needed_to);  // (sums only grow)
         if (i < A.n) {
@@ -194,10 +314,9 @@ __global__ __launch_bounds__(kScanThreads) void sum_requests(prep_block_args A, 
     }
 }
 
-__global__ __launch_bounds__(kThreads) void place_slots(prep_block_args A, const int32_t *__restrict__ starts, const int32_t *__restrict__ taken)
+// Slot of token t; starts and taken as above, or in LDS.
+__device__ __forceinline__ int64_t slot_of(const prep_block_args &A, int64_t t, const int32_t *starts, const int32_t *taken, int32_t on_stack)
 {
-    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (t >= A.capacity) return;
     int64_t slot = -1;
     if (t < starts[A.n]) {
         const int i = last_not_above(starts, A.n, t);
@@ -210,14 +329,95 @@ __global__ __launch_bounds__(kThreads) void place_slots(prep_block_args A, const
             if (block < had) {
                 id = *entry;
             } else {
-                const int32_t on_stack = min(max(*A.free_count, 0), A.free_capacity);
                 id = A.free_blocks[on_stack - 1 - (taken[i] + (int32_t)(block - had))];
                 if (offset == 0) *entry = id;  // the block's first token is a new one
             }
             if (id >= 0 && (int64_t)id < A.n_blocks) slot = (int64_t)id * size + offset;
         }
     }
-    A.slots[t] = slot;
+    return slot;
+}
+
+__global__ __launch_bounds__(kThreads) void place_slots(prep_block_args A, const int32_t *__restrict__ starts, const int32_t *__restrict__ taken)
+{
+    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (t < A.capacity) A.slots[t] = slot_of(A, t, starts, taken, min(max(*A.free_count, 0), A.free_capacity));
+}
+
+// Both in one launch, for at most kListed requests.
+__global__ __launch_bounds__(kListThreads) void place_slots_listed(prep_block_args A)
+{
+    // first tokens of the requests (before: their tokens); blocks off the stack before each, or -1 (before: blocks
+    // that it needs, or -1 = it has tokens but cannot be served)
+    __shared__ alignas(16) int32_t starts[kListed + kPerThread], taken[kListed + kPerThread];
+    __shared__ uint32_t used;
+    const int32_t n = A.n, i0 = (int32_t)threadIdx.x * kPerThread;
+    const int32_t on_stack = min(max(*A.free_count, 0), A.free_capacity);
+    if (threadIdx.x == 0) used = 0;
+    for (int32_t i = threadIdx.x; i < n; i += kListThreads) {
+        int32_t cached = A.cached[i], fresh = A.fresh[i];
+        const bool sound = cached >= 0 && fresh >= 0;
+        if (!sound) cached = fresh = 0;
+        const uint32_t after = (uint32_t)cached + (uint32_t)fresh;
+        const uint32_t had = blocks_of((uint32_t)cached, (uint32_t)A.block_size), want = blocks_of(after, (uint32_t)A.block_size);
+        const bool fits = sound && after <= (uint32_t)INT32_MAX && want <= (uint32_t)A.table_width;
+        starts[i] = fresh;
+        taken[i] = fits ? (int32_t)(want - had) : -1;
+    }
+    __syncthreads();
+    uint64_t tokens = 0, tokens_all, needed = 0, needed_all;
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++)
+        if (i0 + k < n) tokens += (uint64_t)(uint32_t)starts[i0 + k];
+    const uint64_t token0 = scan_block<kListWaves, uint64_t>(tokens, &tokens_all, Sum());
+    {
+        uint64_t token = token0;
+#pragma unroll
+        for (int k = 0; k < kPerThread; k++)
+            if (i0 + k < n) {
+                token += (uint64_t)(uint32_t)starts[i0 + k];
+                if (token > (uint64_t)A.capacity) taken[i0 + k] = -1;
+                if (taken[i0 + k] > 0) needed += (uint64_t)(uint32_t)taken[i0 + k];
+            }
+    }
+    uint64_t block = scan_block<kListWaves, uint64_t>(needed, &needed_all, Sum());
+    {
+        uint64_t token = token0;
+        uint32_t mine = 0;  // blocks off the stack after the thread's last request that takes some
+#pragma unroll
+        for (int k = 0; k < kPerThread; k++)
+            if (i0 + k < n) {
+                const uint64_t fresh = (uint64_t)(uint32_t)starts[i0 + k];
+                const int32_t need = taken[i0 + k];
+                starts[i0 + k] = clip31(token);
+                token += fresh;
+                if (need > 0) {
+                    const bool granted = block + (uint64_t)(uint32_t)need <= (uint64_t)on_stack;
+                    taken[i0 + k] = granted ? (int32_t)block : -1;
+                    block += (uint64_t)(uint32_t)need;
+                    if (granted) mine = (uint32_t)block;
+                }
+            }
+        if (mine != 0) atomicMax(&used, mine);
+    }
+    if (threadIdx.x == 0) starts[n] = clip31(tokens_all);
+    __syncthreads();
+    if (blockIdx.x == 0) {
+        for (int32_t i = threadIdx.x; i <= n; i += kListThreads) {
+            A.token_starts[i] = starts[i];
+            if (i == n) break;
+            const int32_t cached = A.cached[i], fresh = A.fresh[i];
+            const bool sound = cached >= 0 && fresh >= 0, granted = taken[i] >= 0;
+            A.lengths[i] = granted ? cached + fresh : sound ? cached : 0;
+            A.status[i] = granted ? PREP_OK : sound ? PREP_E_TOO_LARGE : PREP_E_INVALID_ARG;
+        }
+        if (threadIdx.x == 0) *A.free_left = on_stack - (int32_t)used;
+    }
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; k++) {
+        const int64_t t = (int64_t)blockIdx.x * kTokensPerWg + k * kListThreads + threadIdx.x;
+        if (t < A.capacity) A.slots[t] = slot_of(A, t, starts, taken, on_stack);
+    }
 }
 
 }  // namespace
@@ -250,6 +450,11 @@ int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n
     const SegmentList L = {segments, seq_segments, first, n_segments, n_seq};
     int32_t *starts = static_cast<int32_t *>(workspace);
     uint32_t *moved = reinterpret_cast<uint32_t *>(starts + n_segments + 1);
+    if (n_segments <= kListed && n_seq <= kListed) {
+        const int64_t blocks = capacity > kTokensPerWg ? (capacity + kTokensPerWg - 1) / kTokensPerWg : 1;
+        hipLaunchKernelGGL(place_listed, dim3((uint32_t)blocks), dim3(kListThreads), 0, stream, L, merge, positions, capacity, token_starts, next);
+        return hipGetLastError() == hipSuccess ? PREP_OK : PREP_E_HIP;
+    }
     hipLaunchKernelGGL(sum_segments, dim3(1), dim3(kScanThreads), 0, stream, L, starts, moved);
     const int64_t items = capacity > n_seq + 1 ? capacity : n_seq + 1;
     hipLaunchKernelGGL(place_tokens, dim3((uint32_t)((items + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, L, merge,
@@ -258,6 +463,8 @@ int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n
 }
 
 uint64_t prep_block_slots_workspace(int32_t n) { return n < 0 || n > kMaxEntries ? 0 : ((uint64_t)n + 1) * 8; }
+
+static_assert(sizeof(prep_block_args) == 136, "as the binding packs it");
 
 int prep_block_slots(int32_t device, const prep_block_args *args, void *stream_ptr)
 {
@@ -268,7 +475,7 @@ int prep_block_slots(int32_t device, const prep_block_args *args, void *stream_p
         A.free_capacity < 0 || A.table_width < 0 || A.table_stride < A.table_width || A.capacity < 0 || A.capacity > 0x7FFFFFFF)
         return PREP_E_INVALID_ARG;
     if ((A.n > 0 && (!A.cached || !A.fresh || !A.lengths || !A.status || (A.table_width > 0 && !A.table))) ||
-        (A.free_capacity > 0 && !A.free_blocks) || !A.free_count || !A.free_left || A.free_left == A.free_count || !A.token_starts ||
+        (A.free_capacity > 0 && !A.free_blocks) || !A.free_count || !A.free_left || A.free_left == A.free_count || (A.n > 0 && (A.lengths == A.cached || A.lengths == A.fresh || A.status == A.cached || A.status == A.fresh)) || !A.token_starts ||
         (A.capacity > 0 && !A.slots) || !A.workspace)
         return PREP_E_INVALID_ARG;
     if (!aligned(A.cached, 4) || !aligned(A.fresh, 4) || !aligned(A.free_blocks, 4) || !aligned(A.free_count, 4) || !aligned(A.table, 4) ||
@@ -279,6 +486,11 @@ int prep_block_slots(int32_t device, const prep_block_args *args, void *stream_p
     DeviceScope scope(device);
     if (!scope.ok()) return PREP_E_HIP;
     int32_t *starts = static_cast<int32_t *>(A.workspace), *taken = starts + A.n + 1;
+    if (A.n <= kListed) {
+        const int64_t blocks = A.capacity > kTokensPerWg ? (A.capacity + kTokensPerWg - 1) / kTokensPerWg : 1;
+        hipLaunchKernelGGL(place_slots_listed, dim3((uint32_t)blocks), dim3(kListThreads), 0, stream, A);
+        return hipGetLastError() == hipSuccess ? PREP_OK : PREP_E_HIP;
+    }
     hipLaunchKernelGGL(sum_requests, dim3(1), dim3(kScanThreads), 0, stream, A, starts, taken);
     if (A.capacity > 0)
         hipLaunchKernelGGL(place_slots, dim3((uint32_t)((A.capacity + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, A,

@@ -413,6 +413,8 @@ int prep_rotary_destroy(prep_rotary *r)
     return PREP_OK;
 }
 
+static_assert(sizeof(prep_rotary_args) == 216, "as the binding packs it");
+
 int prep_rotary_apply(prep_rotary *r, const prep_rotary_args *args, void *stream_ptr)
 {
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);

@@ -33,6 +33,12 @@ def run(*checks):
     assert r.returncode == 0 and r.stdout.endswith("all passed\n"), r.stdout[-500:] + r.stderr[-4000:]
 
 
+def test_argument_blocks_are_packed_as_the_sources_declare_them():
+    import paper_2411_19114_amd.binding as binding
+    for packed, source in ((binding._BLOCK_ARGS, "packing.hip"), (binding._ROTARY_ARGS, "rotary.hip")):
+        assert f"_args) == {packed.size}," in open(os.path.join(emul.CSRC, source)).read()
+
+
 def _some(names, k, of):
     return [n for i, n in enumerate(names) if i % of == k]
 

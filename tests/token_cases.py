@@ -142,6 +142,8 @@ POSITIONS = {
     "no_room": ([[T(5)], [T(2)]], 1, -7, None),
     "wraps": ([[T(6)], [T(2)]], 1, 0, [2 ** 31 - 3, -4]),
     "long_steps": ([[G(3, 1, 2, 32767), T(1)]], 1, 0, None),
+    "long_list": ([[T(i % 2), G(1, 1, 1 + i % 2)] * 50 for i in range(45)], 1, 2, list(range(45))),
+    "many_sequences": ([[T(i % 3)] if i % 5 else [] for i in range(4300)], 1, 0, None),
     "many_segments": ([[T(1 + i % 3), G(1, 1 + i % 2, 2)] * 40 for i in range(30)], 2, 9, list(range(30))),
 }
 
@@ -189,6 +191,7 @@ SLOTS = {
     "too_little_room": ([0, 0, 0], [5, 6, 7], 4, 4, 2, -4),
     "no_room": ([3], [4], 4, 4, 2, -4),
     "negative": ([0, -1, 4, 2 ** 31 - 1], [5, 3, -2, 2], 4, 4, 2, 1),
+    "long_list": ([(i * 7) % 50 for i in range(4200)], [(i * 5) % 3 for i in range(4200)], 4, 16, -3, 5),
     "many": ([(i * 7) % 50 for i in range(1500)], [(i * 5) % 4 for i in range(1500)], 4, 16, 7, 11),
 }
 
@@ -503,7 +506,7 @@ def check_packing_refusals(backend):
     for kw in (dict(n=-1), dict(n=(1 << 20) + 1), dict(block_size=0), dict(block_size=65537), dict(n_blocks=-1), dict(n_blocks=2 ** 31),
                dict(free_capacity=-1), dict(table_width=-1), dict(table_stride=3), dict(capacity=-1), dict(capacity=2 ** 31), dict(cached_ptr=0),
                dict(fresh_ptr=0), dict(free_blocks_ptr=0), dict(free_count_ptr=0), dict(table_ptr=0), dict(slots_ptr=0), dict(token_starts_ptr=0),
-               dict(lengths_ptr=0), dict(status_ptr=0), dict(free_left_ptr=0), dict(free_left_ptr=p + 256), dict(workspace_ptr=0),
+               dict(lengths_ptr=0), dict(status_ptr=0), dict(free_left_ptr=0), dict(free_left_ptr=p + 256), dict(lengths_ptr=p), dict(status_ptr=p + 64), dict(workspace_ptr=0),
                dict(slots_ptr=p + 4), dict(cached_ptr=p + 1), dict(table_ptr=p + 2), dict(workspace_ptr=p + 4)):
         refused(E, prep.block_slots, **{**good, **kw})
     refused(L, prep.block_slots, **{**good, "workspace_bytes": prep.block_slots_workspace(2) - 1})
