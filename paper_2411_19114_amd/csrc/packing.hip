@@ -23,34 +23,52 @@ constexpr int32_t kMaxEntries = 1 << 20;
 constexpr int kListThreads = 512, kListWaves = kListThreads / 64, kListed = 4096, kPerThread = kListed / kListThreads;
 constexpr int kTokensPerThread = 4, kTokensPerWg = kListThreads * kTokensPerThread;
 
-struct Sum {
-    template <typename T> __device__ T operator()(T a, T b) const { return a + b; }
+// What a prefix sum carries: whole numbers that add up, and one of which the largest counts.
+struct Sums {
+    uint64_t tokens;
+    uint64_t blocks;
+    uint32_t moved;
+    uint32_t sequence;
 };
-struct Largest {
-    template <typename T> __device__ T operator()(T a, T b) const { return a < b ? b : a; }
-};
-// v of the lanes before one's own taken together, in a workgroup of kScanWaves waves; *total = of all.  0 is the
-// operation's neutral value.
-template <int kScanWaves, typename T, typename Op>
-__device__ T scan_block(T v, T *total, Op op)
+__device__ __forceinline__ Sums operator+(const Sums &a, const Sums &b)
 {
-    __shared__ T wave_sum[kScanWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int d = 1; d < 64; d *= 2) {
-        const T u = __shfl_up(v, (unsigned)d);
-        if (lane >= d) v = op(u, v);
+    return {a.tokens + b.tokens, a.blocks + b.blocks, a.moved + b.moved, max(a.sequence, b.sequence)};
+}
+// The members that kPlaces names (places) or does not (slots) are left out.
+template <bool kPlaces>
+__device__ __forceinline__ Sums from_lane_before(const Sums &v, unsigned d)
+{
+    Sums r = {__shfl_up(v.tokens, d), 0, 0, 0};
+    if (kPlaces) {
+        r.moved = __shfl_up(v.moved, d);
+        r.sequence = __shfl_up(v.sequence, d);
+    } else {
+        r.blocks = __shfl_up(v.blocks, d);
     }
-    const T left = __shfl_up(v, 1u);
+    return r;
+}
+// v of the lanes before one's own taken together, in a workgroup of kScanWaves waves; *total = of all.
+template <int kScanWaves, bool kPlaces>
+__device__ Sums scan_block(Sums v, Sums *total)
+{
+    __shared__ Sums wave_sum[kScanWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const Sums u = from_lane_before<kPlaces>(v, (unsigned)d);
+        if (lane >= d) v = u + v;
+    }
+    const Sums left = from_lane_before<kPlaces>(v, 1u);
     if (lane == 63) wave_sum[wave] = v;
     __syncthreads();
-    T before = 0, all = 0;
+    Sums before = {0, 0, 0, 0}, all = {0, 0, 0, 0};
     for (int w = 0; w < kScanWaves; w++) {
-        if (w < wave) before = op(before, wave_sum[w]);
-        all = op(all, wave_sum[w]);
+        if (w < wave) before = before + wave_sum[w];
+        all = all + wave_sum[w];
     }
     __syncthreads();
     *total = all;
-    return lane == 0 ? before : op(before, left);
+    return lane == 0 ? before : before + left;
 }
 
 __device__ __forceinline__ int32_t clip31(uint64_t v) { return v > 0x7FFFFFFFull ? 0x7FFFFFFF : (int32_t)v; }
@@ -66,6 +84,23 @@ __device__ __forceinline__ int last_not_above(const int32_t *list, int n, int64_
     }
     return lo;
 }
+
+// The same for kTokens values at once: the searches' reads go out together.  top = the highest power of two below n (0 for
+// n <= 1).
+template <int kTokens>
+__device__ __forceinline__ void search_together(const int32_t *list, int n, int top, const int64_t *v, int *at)
+{
+#pragma unroll
+    for (int k = 0; k < kTokens; k++) at[k] = 0;
+    for (int step = top; step > 0; step >>= 1) {
+#pragma unroll
+        for (int k = 0; k < kTokens; k++) {
+            const int c = at[k] + step;
+            if (c < n && list[min(c, n - 1)] <= v[k]) at[k] = c;
+        }
+    }
+}
+__device__ __forceinline__ int top_step(int n) { return n <= 1 ? 0 : 1 << (31 - __clz(n - 1)); }
 
 // ---- places --------------------------------------------------------------------------------------
 
@@ -96,25 +131,21 @@ __device__ __forceinline__ void segment_size(const prep_segment &s, uint64_t *to
 __global__ __launch_bounds__(kScanThreads) void sum_segments(SegmentList L, int32_t *__restrict__ starts, uint32_t *__restrict__ moved)
 {
     const int32_t lo = seq_bound(L, 0), hi = seq_bound(L, L.n_seq);
-    uint64_t tokens_before = 0;
-    uint32_t moved_before = 0;
+    Sums before = {0, 0, 0, 0};
     for (int32_t at = 0; at < L.n_segments; at += kScanThreads) {
         const int32_t j = at + (int32_t)threadIdx.x;
-        uint64_t tokens = 0, tokens_all;
-        uint32_t advance = 0, moved_all;
-        if (j >= lo && j < hi) segment_size(L.segments[j], &tokens, &advance);
-        const uint64_t token = scan_block<kWaves, uint64_t>(tokens, &tokens_all, Sum());
-        const uint32_t move = scan_block<kWaves, uint32_t>(advance, &moved_all, Sum());
+        Sums mine = {0, 0, 0, 0}, all;
+        if (j >= lo && j < hi) segment_size(L.segments[j], &mine.tokens, &mine.moved);
+        const Sums here = before + scan_block<kWaves, true>(mine, &all);
         if (j < L.n_segments) {
-            starts[j] = clip31(tokens_before + token);
-            moved[j] = moved_before + move;
+            starts[j] = clip31(here.tokens);
+            moved[j] = here.moved;
         }
-        tokens_before += tokens_all;
-        moved_before += moved_all;
+        before = before + all;
     }
     if (threadIdx.x == 0) {
-        starts[L.n_segments] = clip31(tokens_before);
-        moved[L.n_segments] = moved_before;
+        starts[L.n_segments] = clip31(before.tokens);
+        moved[L.n_segments] = before.moved;
     }
 }
 
@@ -177,91 +208,95 @@ __global__ __launch_bounds__(kListThreads) void place_listed(SegmentList L, int3
                                                              int64_t capacity, int32_t *__restrict__ token_starts,
                                                              int32_t *__restrict__ next)
 {
-    // first tokens of the segments; how far places have moved before each; and first the sequence that begins at a
-    // segment (+ 1, 0 = none), then the place where the segment starts
+    // of the segments: the first token (before: tokens), how far places have moved before it (before: its own share),
+    // and its sequence + 1 (before: the sequence that begins there, 0 = none); of the sequences: where places
+    // would start if all of the list's segments were theirs
     __shared__ alignas(16) int32_t starts[kListed + kPerThread];
-    __shared__ alignas(16) uint32_t moved[kListed + kPerThread], base[kListed + kPerThread];
+    __shared__ alignas(16) uint32_t moved[kListed + kPerThread], sequence[kListed + kPerThread], origin[kListed];
     const int32_t n = L.n_segments, lo = seq_bound(L, 0), hi = seq_bound(L, L.n_seq);
-    for (int32_t j = threadIdx.x; j <= n; j += kListThreads) base[j] = 0;
+    // what is read goes out together
+    prep_segment segment[kPerThread];
+    int32_t begins[kPerThread];
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++) {
+        const int32_t e = k * kListThreads + (int32_t)threadIdx.x;
+        segment[k] = prep_segment{0, 0, 0, 0};
+        if (e < n) segment[k] = L.segments[e];
+        if (e < L.n_seq) begins[k] = seq_bound(L, e);
+    }
+    for (int32_t j = threadIdx.x; j <= n; j += kListThreads) sequence[j] = 0;
     __syncthreads();
-    for (int32_t q = threadIdx.x; q < L.n_seq; q += kListThreads) atomicMax(&base[seq_bound(L, q)], (uint32_t)q + 1);
-    for (int32_t j = threadIdx.x; j < n; j += kListThreads) {
-        uint64_t tokens = 0;
-        uint32_t advance = 0;
-        if (j >= lo && j < hi) segment_size(L.segments[j], &tokens, &advance);
-        starts[j] = clip31(tokens);
-        moved[j] = advance;
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++) {
+        const int32_t e = k * kListThreads + (int32_t)threadIdx.x;
+        if (e < L.n_seq) atomicMax(&sequence[begins[k]], (uint32_t)e + 1);
+        if (e < n) {
+            uint64_t tokens = 0;
+            uint32_t advance = 0;
+            if (e >= lo && e < hi) segment_size(segment[k], &tokens, &advance);
+            starts[e] = clip31(tokens);
+            moved[e] = advance;
+        }
     }
     __syncthreads();
     const int32_t j0 = (int32_t)threadIdx.x * kPerThread;
-    uint64_t tokens = 0, tokens_all;
-    uint32_t advance = 0, moved_all, sequence = 0, sequences;
+    Sums mine = {0, 0, 0, 0}, all;
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++)
+        if (j0 + k < n) mine = mine + Sums{(uint64_t)(uint32_t)starts[j0 + k], 0, moved[j0 + k], sequence[j0 + k]};
+    Sums here = scan_block<kListWaves, true>(mine, &all);
 #pragma unroll
     for (int k = 0; k < kPerThread; k++) {
         if (j0 + k < n) {
-            tokens += (uint64_t)(uint32_t)starts[j0 + k];
-            advance += moved[j0 + k];
-            if (base[j0 + k] > sequence) sequence = base[j0 + k];
-        }
-    }
-    uint64_t token = scan_block<kListWaves, uint64_t>(tokens, &tokens_all, Sum());
-    uint32_t move = scan_block<kListWaves, uint32_t>(advance, &moved_all, Sum());
-    uint32_t q = scan_block<kListWaves, uint32_t>(sequence, &sequences, Largest());  // the sequence of the segment before
-#pragma unroll
-    for (int k = 0; k < kPerThread; k++) {
-        if (j0 + k < n) {
-            const uint64_t mine = (uint64_t)(uint32_t)starts[j0 + k];
-            const uint32_t far = moved[j0 + k];
-            starts[j0 + k] = clip31(token);
-            moved[j0 + k] = move;
-            token += mine;
-            move += far;
+            const Sums own = {(uint64_t)(uint32_t)starts[j0 + k], 0, moved[j0 + k], sequence[j0 + k]};
+            starts[j0 + k] = clip31(here.tokens);
+            moved[j0 + k] = here.moved;
+            here = here + own;
+            sequence[j0 + k] = here.sequence;
         }
     }
     if (threadIdx.x == 0) {
-        starts[n] = clip31(tokens_all);
-        moved[n] = moved_all;
+        starts[n] = clip31(all.tokens);
+        moved[n] = all.moved;
     }
     __syncthreads();
-    {
-        uint32_t from = 0;
-        bool known = false;
 #pragma unroll
-        for (int k = 0; k < kPerThread; k++) {
-            if (j0 + k < n) {
-                if (base[j0 + k] != 0) {
-                    q = base[j0 + k];
-                    known = false;
-                }
-                if (!known && q != 0) {
-                    from = (L.first ? (uint32_t)L.first[q - 1] : 0u) - moved[seq_bound(L, (int)q - 1)];
-                    known = true;
-                }
-                base[j0 + k] = from + moved[j0 + k];
-            }
-        }
+    for (int k = 0; k < kPerThread; k++) {
+        const int32_t q = k * kListThreads + (int32_t)threadIdx.x;
+        if (q < L.n_seq) origin[q] = (L.first ? (uint32_t)L.first[q] : 0u) - moved[begins[k]];
+    }
+    // the sequences' own results, dealt to the workgroups
+    for (int32_t q = (int32_t)(blockIdx.x * kListThreads + threadIdx.x); q <= L.n_seq; q += (int32_t)(gridDim.x * kListThreads)) {
+        const int32_t b = seq_bound(L, q);
+        token_starts[q] = starts[b];
+        if (next != nullptr && q < L.n_seq) next[q] = (int32_t)((L.first ? (uint32_t)L.first[q] : 0u) + moved[seq_bound(L, q + 1)] - moved[b]);
     }
     __syncthreads();
-    if (blockIdx.x == 0)
-        for (int32_t q = threadIdx.x; q <= L.n_seq; q += kListThreads) {
-            const int32_t b = seq_bound(L, q);
-            token_starts[q] = starts[b];
-            if (next != nullptr && q < L.n_seq) next[q] = (int32_t)((L.first ? (uint32_t)L.first[q] : 0u) + moved[seq_bound(L, q + 1)] - moved[b]);
-        }
+    const int64_t token0 = (int64_t)blockIdx.x * kTokensPerWg + threadIdx.x;
+    int64_t token[kTokensPerThread];
+    int at[kTokensPerThread];
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; k++) token[k] = token0 + k * kListThreads;
+    search_together<kTokensPerThread>(starts, n, top_step(n), token, at);
+    const int32_t total = starts[n];
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; k++) segment[k] = token[k] < total ? L.segments[at[k]] : prep_segment{0, 0, 0, 0};
 #pragma unroll
     for (int k = 0; k < kTokensPerThread; k++) {
-        const int64_t i = (int64_t)blockIdx.x * kTokensPerWg + k * kListThreads + threadIdx.x;
-        if (i >= capacity) break;
+        if (token[k] >= capacity) break;
         Place p = {0, 0, 0};
-        if (i < starts[n]) {
-            const int j = last_not_above(starts, n, i);
-            p = place_in_segment(L.segments[j], base[j], (uint32_t)i - (uint32_t)starts[j], merge);
+        if (token[k] < total) {
+            const int j = at[k];
+            const uint32_t q = sequence[j];  // (not 0 where a segment has tokens)
+            const uint32_t base = (q != 0 ? origin[q - 1] : 0u) + moved[j];
+            p = place_in_segment(segment[k], base, (uint32_t)token[k] - (uint32_t)starts[j], merge);
         }
-        positions[i] = (int32_t)p.t;
-        positions[capacity + i] = (int32_t)p.h;
-        positions[2 * capacity + i] = (int32_t)p.w;
+        positions[token[k]] = (int32_t)p.t;
+        positions[capacity + token[k]] = (int32_t)p.h;
+        positions[2 * capacity + token[k]] = (int32_t)p.w;
     }
 }
+static_assert(kTokensPerThread <= kPerThread, "place_listed keeps the tokens' segments where it kept the list's");
 
 // ---- slots ---------------------------------------------------------------------------------------
 
@@ -272,151 +307,164 @@ __device__ __forceinline__ uint32_t blocks_of(uint32_t v, uint32_t block_size)
     return whole + (whole * block_size != v ? 1u : 0u);
 }
 
-// starts[i]: first token of request i, n + 1 entries; taken[i]: blocks off the stack before its own, or -1: it is refused.
+// Tokens of request i, and the blocks that it needs; false = it cannot be served whatever there is (or is no request).
+// Of the requests before, all count: once a sum of tokens is beyond the capacity, or a sum of blocks beyond the stack, so
+// are the later ones, and what is refused changes nothing for them.
+__device__ __forceinline__ bool request_needs(const prep_block_args &A, int32_t cached, int32_t fresh, uint32_t *tokens, uint32_t *blocks)
+{
+    *tokens = *blocks = 0;
+    if (cached < 0 || fresh < 0) return false;
+    *tokens = (uint32_t)fresh;
+    const uint32_t after = (uint32_t)cached + (uint32_t)fresh;
+    const uint32_t want = blocks_of(after, (uint32_t)A.block_size);
+    if (after > (uint32_t)INT32_MAX || want > (uint32_t)A.table_width) return false;
+    *blocks = want - blocks_of((uint32_t)cached, (uint32_t)A.block_size);
+    return true;
+}
+// Blocks off the stack before a request's own, or -1: it is refused.
+__device__ __forceinline__ int32_t grant(const prep_block_args &A, const Sums &before, uint32_t tokens, uint32_t blocks, int32_t on_stack)
+{
+    if (before.tokens + tokens > (uint64_t)A.capacity) return -1;
+    if (blocks == 0) return 0;
+    return before.blocks + blocks <= (uint64_t)on_stack ? (int32_t)before.blocks : -1;
+}
+__device__ __forceinline__ void report_request(const prep_block_args &A, int32_t i, int32_t cached, int32_t fresh, bool granted)
+{
+    const bool sound = cached >= 0 && fresh >= 0;
+    A.lengths[i] = granted ? cached + fresh : sound ? cached : 0;
+    A.status[i] = granted ? PREP_OK : sound ? PREP_E_TOO_LARGE : PREP_E_INVALID_ARG;
+}
+
+// starts[i]: first token of request i, n + 1 entries; taken[i]: as grant gives it.
 __global__ __launch_bounds__(kScanThreads) void sum_requests(prep_block_args A, int32_t *__restrict__ starts, int32_t *__restrict__ taken)
 {
     __shared__ uint32_t used;  // blocks that go
     if (threadIdx.x == 0) used = 0;
     const int32_t on_stack = min(max(*A.free_count, 0), A.free_capacity);
-    uint64_t tokens_before = 0, needed_before = 0;
+    Sums before = {0, 0, 0, 0};
     for (int32_t at = 0; at < A.n; at += kScanThreads) {
         const int32_t i = at + (int32_t)threadIdx.x;
-        int32_t cached = 0, fresh = 0;
-        bool sound = i < A.n;
-        if (sound) {
-            cached = A.cached[i];
-            fresh = A.fresh[i];
-            sound = cached >= 0 && fresh >= 0;
-            if (!sound) cached = fresh = 0;
-        }
-        uint64_t tokens_all, needed_all;
-        const uint64_t tokens_to = tokens_before + scan_block<kWaves, uint64_t>((uint64_t)fresh, &tokens_all, Sum()) + (uint64_t)fresh;
-        const uint32_t after = (uint32_t)cached + (uint32_t)fresh;
-        const uint32_t had = blocks_of((uint32_t)cached, (uint32_t)A.block_size), want = blocks_of(after, (uint32_t)A.block_size);
-        const bool fits = sound && after <= (uint32_t)INT32_MAX && want <= (uint32_t)A.table_width && tokens_to <= (uint64_t)A.capacity;
-        const uint32_t need = fits ? want - had : 0;
-        const uint64_t needed_to = needed_before + scan_block<kWaves, uint64_t>(need, &needed_all, Sum()) + need;
-        const bool granted = fits && (need == 0 || needed_to <= (uint64_t)on_stack);
-        if (granted && need != 0) atomicMax(&used, (uint32_t)needed_to);  // (sums only grow)
+        const int32_t cached = i < A.n ? A.cached[i] : -1, fresh = i < A.n ? A.fresh[i] : -1;
+        uint32_t tokens, blocks;
+        const bool fits = request_needs(A, cached, fresh, &tokens, &blocks);
+        Sums all;
+        const Sums here = before + scan_block<kWaves, false>(Sums{tokens, blocks, 0, 0}, &all);
+        const int32_t given = fits ? grant(A, here, tokens, blocks, on_stack) : -1;
+        if (given >= 0 && blocks != 0) atomicMax(&used, (uint32_t)given + blocks);  // (sums only grow)
         if (i < A.n) {
-            starts[i] = A.token_starts[i] = clip31(tokens_to - (uint64_t)fresh);
-            taken[i] = !granted ? -1 : need == 0 ? 0 : (int32_t)(needed_to - need);
-            A.lengths[i] = granted ? (int32_t)after : cached;
-            A.status[i] = granted ? PREP_OK : sound ? PREP_E_TOO_LARGE : PREP_E_INVALID_ARG;
+            starts[i] = A.token_starts[i] = clip31(here.tokens);
+            taken[i] = given;
+            report_request(A, i, cached, fresh, given >= 0);
         }
-        tokens_before += tokens_all;
-        needed_before += needed_all;
+        before = before + all;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        starts[A.n] = A.token_starts[A.n] = clip31(tokens_before);
+        starts[A.n] = A.token_starts[A.n] = clip31(before.tokens);
         *A.free_left = on_stack - (int32_t)used;
     }
 }
 
-// Slot of token t; starts and taken as above, or in LDS.
-__device__ __forceinline__ int64_t slot_of(const prep_block_args &A, int64_t t, const int32_t *starts, const int32_t *taken, int32_t on_stack)
+// Slot of token t of a request that is served: blocks taken before its own, its first token.
+__device__ __forceinline__ int64_t slot_of(const prep_block_args &A, int32_t i, uint32_t cached, uint32_t r, int32_t taken, int32_t on_stack)
 {
-    int64_t slot = -1;
-    if (t < starts[A.n]) {
-        const int i = last_not_above(starts, A.n, t);
-        if (taken[i] >= 0) {
-            const uint32_t cached = (uint32_t)A.cached[i], size = (uint32_t)A.block_size;
-            const uint32_t place = cached + (uint32_t)t - (uint32_t)starts[i];
-            const uint32_t block = place / size, had = blocks_of(cached, size), offset = place - block * size;
-            int32_t *entry = A.table + (int64_t)i * A.table_stride + block;
-            int32_t id;
-            if (block < had) {
-                id = *entry;
-            } else {
-                id = A.free_blocks[on_stack - 1 - (taken[i] + (int32_t)(block - had))];
-                if (offset == 0) *entry = id;  // the block's first token is a new one
-            }
-            if (id >= 0 && (int64_t)id < A.n_blocks) slot = (int64_t)id * size + offset;
-        }
+    const uint32_t size = (uint32_t)A.block_size, place = cached + r;
+    const uint32_t block = place / size, had = blocks_of(cached, size), offset = place - block * size;
+    int32_t *entry = A.table + (int64_t)i * A.table_stride + block;
+    int32_t id;
+    if (block < had) {
+        id = *entry;
+    } else {
+        id = A.free_blocks[on_stack - 1 - (taken + (int32_t)(block - had))];
+        if (offset == 0) *entry = id;  // the block's first token is a new one
     }
-    return slot;
+    return id >= 0 && (int64_t)id < A.n_blocks ? (int64_t)id * size + offset : -1;
 }
 
 __global__ __launch_bounds__(kThreads) void place_slots(prep_block_args A, const int32_t *__restrict__ starts, const int32_t *__restrict__ taken)
 {
     const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (t < A.capacity) A.slots[t] = slot_of(A, t, starts, taken, min(max(*A.free_count, 0), A.free_capacity));
+    if (t >= A.capacity) return;
+    int64_t slot = -1;
+    if (t < starts[A.n]) {
+        const int i = last_not_above(starts, A.n, t);
+        if (taken[i] >= 0)
+            slot = slot_of(A, i, (uint32_t)A.cached[i], (uint32_t)t - (uint32_t)starts[i], taken[i], min(max(*A.free_count, 0), A.free_capacity));
+    }
+    A.slots[t] = slot;
 }
 
 // Both in one launch, for at most kListed requests.
 __global__ __launch_bounds__(kListThreads) void place_slots_listed(prep_block_args A)
 {
-    // first tokens of the requests (before: their tokens); blocks off the stack before each, or -1 (before: blocks
-    // that it needs, or -1 = it has tokens but cannot be served)
+    // of the requests: the first token (before: tokens), and blocks taken before its own or -1 (before: the blocks
+    // that it needs or -1)
     __shared__ alignas(16) int32_t starts[kListed + kPerThread], taken[kListed + kPerThread];
     __shared__ uint32_t used;
     const int32_t n = A.n, i0 = (int32_t)threadIdx.x * kPerThread;
     const int32_t on_stack = min(max(*A.free_count, 0), A.free_capacity);
     if (threadIdx.x == 0) used = 0;
-    for (int32_t i = threadIdx.x; i < n; i += kListThreads) {
-        int32_t cached = A.cached[i], fresh = A.fresh[i];
-        const bool sound = cached >= 0 && fresh >= 0;
-        if (!sound) cached = fresh = 0;
-        const uint32_t after = (uint32_t)cached + (uint32_t)fresh;
-        const uint32_t had = blocks_of((uint32_t)cached, (uint32_t)A.block_size), want = blocks_of(after, (uint32_t)A.block_size);
-        const bool fits = sound && after <= (uint32_t)INT32_MAX && want <= (uint32_t)A.table_width;
-        starts[i] = fresh;
-        taken[i] = fits ? (int32_t)(want - had) : -1;
+    int32_t cached[kPerThread], fresh[kPerThread];  // (the reads go out together)
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++) {
+        const int32_t i = k * kListThreads + (int32_t)threadIdx.x;
+        cached[k] = i < n ? A.cached[i] : -1;
+        fresh[k] = i < n ? A.fresh[i] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kPerThread; k++) {
+        const int32_t i = k * kListThreads + (int32_t)threadIdx.x;
+        if (i < n) {
+            uint32_t tokens, blocks;
+            const bool fits = request_needs(A, cached[k], fresh[k], &tokens, &blocks);
+            starts[i] = (int32_t)tokens;
+            taken[i] = fits ? (int32_t)blocks : -1;
+        }
     }
     __syncthreads();
-    uint64_t tokens = 0, tokens_all, needed = 0, needed_all;
+    Sums mine = {0, 0, 0, 0}, all;
 #pragma unroll
     for (int k = 0; k < kPerThread; k++)
-        if (i0 + k < n) tokens += (uint64_t)(uint32_t)starts[i0 + k];
-    const uint64_t token0 = scan_block<kListWaves, uint64_t>(tokens, &tokens_all, Sum());
-    {
-        uint64_t token = token0;
+        if (i0 + k < n) mine = mine + Sums{(uint64_t)(uint32_t)starts[i0 + k], (uint64_t)(uint32_t)max(taken[i0 + k], 0), 0, 0};
+    Sums here = scan_block<kListWaves, false>(mine, &all);
+    uint32_t most = 0;  // blocks off the stack after the thread's last request that takes some
 #pragma unroll
-        for (int k = 0; k < kPerThread; k++)
-            if (i0 + k < n) {
-                token += (uint64_t)(uint32_t)starts[i0 + k];
-                if (token > (uint64_t)A.capacity) taken[i0 + k] = -1;
-                if (taken[i0 + k] > 0) needed += (uint64_t)(uint32_t)taken[i0 + k];
-            }
-    }
-    uint64_t block = scan_block<kListWaves, uint64_t>(needed, &needed_all, Sum());
-    {
-        uint64_t token = token0;
-        uint32_t mine = 0;  // blocks off the stack after the thread's last request that takes some
-#pragma unroll
-        for (int k = 0; k < kPerThread; k++)
-            if (i0 + k < n) {
-                const uint64_t fresh = (uint64_t)(uint32_t)starts[i0 + k];
-                const int32_t need = taken[i0 + k];
-                starts[i0 + k] = clip31(token);
-                token += fresh;
-                if (need > 0) {
-                    const bool granted = block + (uint64_t)(uint32_t)need <= (uint64_t)on_stack;
-                    taken[i0 + k] = granted ? (int32_t)block : -1;
-                    block += (uint64_t)(uint32_t)need;
-                    if (granted) mine = (uint32_t)block;
-                }
-            }
-        if (mine != 0) atomicMax(&used, mine);
-    }
-    if (threadIdx.x == 0) starts[n] = clip31(tokens_all);
-    __syncthreads();
-    if (blockIdx.x == 0) {
-        for (int32_t i = threadIdx.x; i <= n; i += kListThreads) {
-            A.token_starts[i] = starts[i];
-            if (i == n) break;
-            const int32_t cached = A.cached[i], fresh = A.fresh[i];
-            const bool sound = cached >= 0 && fresh >= 0, granted = taken[i] >= 0;
-            A.lengths[i] = granted ? cached + fresh : sound ? cached : 0;
-            A.status[i] = granted ? PREP_OK : sound ? PREP_E_TOO_LARGE : PREP_E_INVALID_ARG;
+    for (int k = 0; k < kPerThread; k++) {
+        if (i0 + k < n) {
+            const uint32_t tokens = (uint32_t)starts[i0 + k], blocks = (uint32_t)max(taken[i0 + k], 0);
+            const int32_t given = taken[i0 + k] >= 0 ? grant(A, here, tokens, blocks, on_stack) : -1;
+            if (given >= 0 && blocks != 0) most = (uint32_t)given + blocks;
+            starts[i0 + k] = clip31(here.tokens);
+            taken[i0 + k] = given;
+            here = here + Sums{tokens, blocks, 0, 0};
         }
-        if (threadIdx.x == 0) *A.free_left = on_stack - (int32_t)used;
     }
+    if (most != 0) atomicMax(&used, most);
+    if (threadIdx.x == 0) starts[n] = clip31(all.tokens);
+    __syncthreads();
+    const int64_t token0 = (int64_t)blockIdx.x * kTokensPerWg + threadIdx.x;
+    int64_t token[kTokensPerThread];
+    int at[kTokensPerThread];
+    int32_t length[kTokensPerThread];
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; k++) token[k] = token0 + k * kListThreads;
+    search_together<kTokensPerThread>(starts, n, top_step(n), token, at);
+    const int32_t total = starts[n];
+#pragma unroll
+    for (int k = 0; k < kTokensPerThread; k++) length[k] = token[k] < total ? A.cached[at[k]] : 0;
 #pragma unroll
     for (int k = 0; k < kTokensPerThread; k++) {
-        const int64_t t = (int64_t)blockIdx.x * kTokensPerWg + k * kListThreads + threadIdx.x;
-        if (t < A.capacity) A.slots[t] = slot_of(A, t, starts, taken, on_stack);
+        if (token[k] >= A.capacity) break;
+        int64_t slot = -1;
+        if (token[k] < total && taken[at[k]] >= 0)
+            slot = slot_of(A, at[k], (uint32_t)length[k], (uint32_t)token[k] - (uint32_t)starts[at[k]], taken[at[k]], on_stack);
+        A.slots[token[k]] = slot;
+    }
+    // the requests' own results, dealt to the workgroups
+    for (int32_t i = (int32_t)(blockIdx.x * kListThreads + threadIdx.x); i <= n; i += (int32_t)(gridDim.x * kListThreads)) {
+        A.token_starts[i] = starts[i];
+        if (i < n) report_request(A, i, A.cached[i], A.fresh[i], taken[i] >= 0);
+        else *A.free_left = on_stack - (int32_t)used;
     }
 }
 

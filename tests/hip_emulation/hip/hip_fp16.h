@@ -39,19 +39,3 @@ inline __half __float2half_rn(float f)
     return __half{h};
 }
 inline __half2 __floats2half2_rn(float a, float b) { return __half2{__float2half_rn(a), __float2half_rn(b)}; }
-inline float __half2float(__half h)
-{
-    const uint32_t sign = (uint32_t)(h.x & 0x8000u) << 16, exp = (h.x >> 10) & 31u, man = h.x & 0x3FFu;
-    float f;
-    if (exp == 0) {
-        f = (float)man * (1.0f / 16777216.0f);
-        uint32_t b;
-        memcpy(&b, &f, 4);
-        b |= sign;
-        memcpy(&f, &b, 4);
-        return f;
-    }
-    const uint32_t b = sign | (exp == 31 ? 0x7F800000u : (exp + 112u) << 23) | (man << 13);
-    memcpy(&f, &b, 4);
-    return f;
-}

@@ -35,10 +35,7 @@ struct dim3 {
 };
 struct uint2 { uint32_t x, y; };
 struct uint4 { uint32_t x, y, z, w; };
-struct float2 { float x, y; };
 struct float4 { float x, y, z, w; };
-struct int4 { int32_t x, y, z, w; };
-inline int4 make_int4(int32_t x, int32_t y, int32_t z, int32_t w) { return {x, y, z, w}; }
 inline uint4 make_uint4(uint32_t x, uint32_t y, uint32_t z, uint32_t w) { return {x, y, z, w}; }
 inline float4 make_float4(float x, float y, float z, float w) { return {x, y, z, w}; }
 
@@ -192,12 +189,6 @@ inline uint32_t atomicCAS(uint32_t *p, uint32_t expected, uint32_t v)
     return expected;
 }
 inline uint32_t atomicAdd(uint32_t *p, uint32_t v) { return __atomic_fetch_add(p, v, __ATOMIC_SEQ_CST); }
-inline uint32_t atomicMax(uint32_t *p, uint32_t v)
-{
-    uint32_t old = __atomic_load_n(p, __ATOMIC_SEQ_CST);
-    while (old < v && !__atomic_compare_exchange_n(p, &old, v, false, __ATOMIC_SEQ_CST, __ATOMIC_SEQ_CST)) {}
-    return old;
-}
 inline int32_t atomicMin(int32_t *p, int32_t v)
 {
     int32_t old = __atomic_load_n(p, __ATOMIC_SEQ_CST);
@@ -252,7 +243,6 @@ template <typename T> inline T max(T a, T b) { return a < b ? b : a; }
 
 // ---- runtime API: the "device" is the host heap --------------------------------------
 inline hipError_t hipGetDeviceCount(int *n) { *n = 1; return hipSuccess; }
-inline hipError_t hipGetDevice(int *d) { *d = 0; return hipSuccess; }
 inline hipError_t hipSetDevice(int) { return hipSuccess; }
 inline hipError_t hipGetLastError() { return hipSuccess; }
 inline hipError_t hipDeviceSynchronize() { return hipSuccess; }

@@ -17,11 +17,11 @@ SOURCES = emul.KERNELS + [k for k in ("patches.hip", "packing.hip", "rotary.hip"
 def build():
     srcs = [os.path.join(emul.CSRC, k) for k in SOURCES] + [os.path.join(emul.EMU, "emul_runtime.cpp")]
     deps = srcs + [os.path.join(emul.CSRC, x) for x in ("kernels.h", "parser.h", "prep_internal.h", "tokens.h")] + \
-        [os.path.join(emul.ROOT, "include", "prep.h")] + [os.path.join(emul.EMU, "hip", x) for x in os.listdir(os.path.join(emul.EMU, "hip"))]
+        [os.path.join(emul.ROOT, "include", "prep.h"), os.path.join(emul.EMU, "more_hip.h")] + [os.path.join(emul.EMU, "hip", x) for x in os.listdir(os.path.join(emul.EMU, "hip"))]
     if os.path.exists(LIBRARY) and os.path.getmtime(LIBRARY) >= max(os.path.getmtime(d) for d in deps):
         return
     subprocess.run(["g++", "-std=c++20", "-O1", "-g", "-pthread", "-fPIC", "-shared", "-fsanitize=address,undefined",
-                    "-fno-sanitize-recover=undefined", "-I", emul.EMU, "-x", "c++"] + srcs + ["-o", LIBRARY], check=True)
+                    "-fno-sanitize-recover=undefined", "-I", emul.EMU, "-include", os.path.join(emul.EMU, "more_hip.h"), "-x", "c++"] + srcs + ["-o", LIBRARY], check=True)
 
 
 def run(*checks):
