@@ -28,3 +28,11 @@ inline uint32_t atomicMax(uint32_t *p, uint32_t v)
 inline int __clz(int v) { return v == 0 ? 32 : __builtin_clz((unsigned)v); }
 
 inline hipError_t hipGetDevice(int *d) { *d = 0; return hipSuccess; }
+
+#define __builtin_amdgcn_fence(...) ((void)0)
+// all lanes of the wave come here
+inline void __builtin_amdgcn_wave_barrier()
+{
+    hip_emul::ThreadState &t = hip_emul::tls;
+    t.ctx->wave_bar[t.tid.x >> 6]->arrive_and_wait();
+}

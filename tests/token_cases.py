@@ -54,6 +54,12 @@ PATCHES = {
     "patch_of_one": ([(9, 7)], [1], 1, 3, 1, "f32", True, 0, 0),
     "large_patch": ([(70, 60)], [1], 64, 1, 1, "bf16", True, 0, 0),
     "more_than_a_launch": ([(4 + i % 5, 4 + i % 3) for i in range(35)], [1] * 35, 4, 1, 1, "f16", True, 0, 0),
+    "several_tiles": ([(203, 90), (90, 203)], [1, 2], 14, 2, 2, "bf16", True, 0, 0),
+    "several_tiles_reduced": ([(310, 190)], [1], 7, 3, 1, "f16", True, 0, 120 * 120),
+    "several_tiles_two_taps": ([(150, 131)], [1], 16, 1, 1, "f32", False, 0, 100 * 100),
+    "tall_patches": ([(150, 200)], [1], 50, 1, 2, "f16", True, 0, 0),
+    "reduced_beyond_tiles": ([(400, 60), (40, 400)], [1, 1], 2, 1, 1, "f32", True, 0, 40),
+    "few_columns": ([(7, 40), (6, 50), (5, 33), (8, 20)], [1] * 4, 4, 1, 1, "f16", True, 0, 0),
     "wide_window": ([(50, 46)], [1], 3, 5, 1, "f32", True, 0, 0),
 }
 
