@@ -4,9 +4,11 @@
 // centre c = (i + 1/2) in / out - 1/2, weights max(0, 1 - |j - c| / s) scaled to sum 1 over the samples inside the image, s =
 // max(in / out, 1) (antialiased) or 1, which is two taps; a tap that the border would clamp counts for the border's sample either way.
 //
-// A workgroup makes a tile of patches: the source samples under the tile go to LDS, every wave sums a row's samples over the
-// rows of its window (weights by row, whole bytes eight at a time), then over the columns, and leaves the values in LDS in the order
-// of the patch rows, from where they are written in runs.
+// A workgroup makes a tile of patches, up to 16 x 64 pixels.  The source samples under it go to LDS.  The sums over rows are a
+// product (16 output rows) x (source rows) x (bytes of a row) on the matrix cores: a byte is a half exactly, a weight is two halves,
+// 2^15 w = hi + lo with 22 bits, and sums are fp32; with vector instructions (a conversion and a multiply-add per tap and byte) that part alone
+// took as long as the rest of the kernel.  The sums over columns are vector instructions, a lane an output column whose weights stay in registers.
+// The values go to LDS in the order of the patch rows, from where they are written in runs.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <cmath>
@@ -16,6 +18,7 @@
 
 #include "../../include/prep.h"
 #include "kernels.h"
+#include "matrix.h"
 #include "tokens.h"
 
 namespace prep {
@@ -26,12 +29,33 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kClips = 32;  // clips of one launch: their records are kernel arguments (3 KB), so that a call has
                             // no workspace, calls may overlap and a captured call keeps its own
 
-// A tile's limits: pixels a side, pixels in all by element size, bytes of source samples, source samples of a row, taps of a row.
-constexpr int kTileCols = 64, kTileRows = 32, kRawBytes = 18 << 10, kSpan = 150, kTaps = 32;
-constexpr int stage_pixels(int element) { return element == 2 ? 2048 : 1024; }
-constexpr int kPatches = 1024;      // of a tile (patches of few pixels)
-constexpr int kLoads = 5;           // 16-byte reads of a thread that go out together
-constexpr int kNarrowest = 6;       // narrowest image whose rows hold a read of 16 bytes
+// Division by a number that the host knows: the quotient by a multiplication is right or one too large.
+struct Divisor {
+    uint32_t d, m;  // m = 2^32 / d, rounded up (d = 1: not looked at)
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const
+    {
+        const uint32_t q = __umulhi(n, m);
+        return d == 1 ? n : q - (q * d > n ? 1u : 0u);
+    }
+};
+inline Divisor divisor(int d) { return {(uint32_t)d, (uint32_t)((0x100000000ull + (uint64_t)d - 1) / (uint64_t)d)}; }
+
+// A tile's limits, for clips whose windows hold at most kFewTaps columns (kWide = false) and for the others.
+constexpr int kTileCols = 64, kTileRows = 16, kPatches = 128;
+constexpr int kStrip = 4;                          // tiles one below the other that a workgroup takes, at most
+constexpr int kNarrowest = 6;                      // narrowest image whose rows hold a read of 16 bytes
+constexpr int kFewTaps = 3, kSomeTaps = 6;          // columns of a window whose weights stay in registers
+constexpr float kWeightScale = 32768.0f;
+template <bool kWide, int kElement>
+struct Limits {
+    static constexpr int span_bytes = kWide ? 448 : 256, sum_pitch = span_bytes + 4;  // of a source row
+    static constexpr int steps = kWide ? 2 : 1, source_rows = 32 * steps;  // products over 32 source rows each
+    // source samples, rows 16-byte multiples apart; the values for the patch rows afterwards
+    static constexpr int raw_bytes = kWide ? 16 << 10 : kElement == 2 ? 8 << 10 : 12 << 10;
+    static constexpr int loads = raw_bytes / (16 * kThreads);  // 16-byte reads of a thread
+    static constexpr int workgroups = kWide ? 3 : kElement == 2 ? 5 : 4;  // that a compute unit's LDS holds
+    static_assert(kTileCols * kTileRows * 3 * kElement <= raw_bytes, "the values take the samples' place");
+};
 
 // One clip as the kernels see it.
 struct PatchClip {
@@ -40,20 +64,25 @@ struct PatchClip {
     int64_t row0;           // its first row
     double scale_x, scale_y;  // source samples per output sample
     uint32_t pitch;
-    int32_t width, height, out_w, out_h;  // pixels
+    int32_t width, height;  // pixels
+    int32_t cols, rows;     // patches
     int32_t frames;
     int32_t image;          // index into `status`
     // tiles: patches across and down, rows of a patch in it (fewer than the patch has where that is tall: `parts` tiles
-    // share a patch then), tiles across and down
+    // share a patch then), tiles across and down; strips of tiles across and down
     int32_t across, down, part_rows, parts, tiles_x, tiles_y;
+    Divisor strips_x, strips;  // in a row of them; of a frame group
 };
 struct ClipPack {
     uint32_t block0[kClips];  // first workgroup of each clip; of those that the launch lacks 2^32 - 1
     PatchClip c[kClips];
 };
+static_assert(sizeof(ClipPack) <= 3968, "kernel arguments are 4 KB at most");
 struct PatchGeometry {
     int32_t patch, merge, group;  // pixels, patches, frames
     int32_t antialias;
+    int32_t strip;                // tiles of a workgroup
+    Divisor by_patch, by_merge;
     float scale[3], bias[3];      // 1 / (255 std), -mean / std
 };
 
@@ -85,28 +114,28 @@ __device__ __forceinline__ int clip_of(const ClipPack &pack, uint32_t block)
     return i;
 }
 
-// Row, inside its group of frames, of patch (py, px).
-__device__ __forceinline__ int row_of_patch(int py, int px, int cols, int merge)
+// Row, inside its group of frames, of patch (py, px): row_of_line(py) + row_of_column(px).
+__device__ __forceinline__ int row_of_line(const PatchGeometry &g, int py, int cols)
 {
-    const int band = py / merge, window = px / merge;
-    return band * merge * cols + window * merge * merge + (py - band * merge) * merge + (px - window * merge);
+    const int band = (int)g.by_merge.quotient((uint32_t)py);
+    return band * g.merge * cols + (py - band * g.merge) * g.merge;
+}
+__device__ __forceinline__ int row_of_column(const PatchGeometry &g, int px)
+{
+    const int window = (int)g.by_merge.quotient((uint32_t)px);
+    return window * g.merge * g.merge + (px - window * g.merge);
 }
 
-// What a wave's lanes have written to LDS is there for all of them.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
+// A value that all lanes of a wave hold alike.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// 16 bytes at `at` of a row of `bytes` (at least 16) bytes, those behind the row's end 0: nothing outside the row is read.
-__device__ __forceinline__ uint4 load_inside(const uint8_t *row, int at, int bytes)
+// The most columns (or rows) that a window holds.
+__host__ __device__ __forceinline__ int columns_of_window(double scale, bool antialias) { return antialias && scale > 1.0 ? (int)(2.0 * scale) + 1 : 2; }
+
+// 16 bytes of a row that were read `back` bytes early, so as to end with the row: those behind the row's end become 0.
+__device__ __forceinline__ uint4 moved_back(uint4 v, int back)
 {
-    uint64_t lo, hi;
-    const int from = min(at, bytes - 16), back = at - from;
-    __builtin_memcpy(&lo, row + from, 8);
-    __builtin_memcpy(&hi, row + from + 8, 8);
+    uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
     if (back != 0) {
         if (back >= 8) {
             lo = hi;
@@ -129,7 +158,7 @@ template <> struct Chunk<2> { typedef uint16_t type; };
 
 // A frame's runs of `run` elements, `n` of them (three of a patch), from the stage to the patches' rows, kBytes at a time.
 template <typename T, int kBytes>
-__device__ __forceinline__ void write_runs(const T *stage, const int32_t *row, int n, int run, T *out, int64_t out_stride, int64_t channel_stride)
+__device__ __forceinline__ void write_runs(const T *stage, const int32_t *row, int n, int run, T *out, int64_t out_stride, int channel_stride)
 {
     typedef typename Chunk<kBytes>::type C;
     constexpr int kElements = kBytes / (int)sizeof(T);
@@ -148,153 +177,261 @@ __device__ __forceinline__ void write_runs(const T *stage, const int32_t *row, i
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void patch_rows_tiled(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
+// Sums over the columns of a lane's window, kTaps samples wide, weights in registers; kTaps = 0: any width, weights formed again for each row.
+template <typename T, int kTaps, int kSumPitch>
+__device__ __forceinline__ void sum_columns(const float *summed, T *stage, const int32_t *row_stage, int tile_h, int x, int first, int taps, float centre,
+                                            float inv, float norm, int most, int run, const PatchGeometry &g)
+{
+    // a window starts earlier where kTaps samples would end behind the row's sums; what is not under the triangle has weight 0
+    const int at = kTaps != 0 ? min(first, most - kTaps) : first;
+    float w[kTaps != 0 ? kTaps : 1];
+#pragma unroll
+    for (int k = 0; k < kTaps; k++) {
+        const int tap = at + k - first;
+        w[k] = tap >= 0 && tap < taps ? fmaxf(0.0f, fmaf(-fabsf((float)tap - centre), inv, 1.0f)) * norm : 0.0f;
+    }
+    for (int t = (int)threadIdx.x >> 6; t < tile_h; t += kWaves) {
+        const float *s = summed + t * kSumPitch + at * 3;
+        float v[3] = {0.0f, 0.0f, 0.0f};
+        if (kTaps != 0) {
+#pragma unroll
+            for (int k = 0; k < kTaps; k++)
+#pragma unroll
+                for (int c = 0; c < 3; c++) v[c] = fmaf(w[k], s[3 * k + c], v[c]);
+        } else {
+            for (int k = 0; k < taps; k++) {
+                const float wk = fmaxf(0.0f, fmaf(-fabsf((float)k - centre), inv, 1.0f)) * norm;
+#pragma unroll
+                for (int c = 0; c < 3; c++) v[c] = fmaf(wk, s[3 * k + c], v[c]);
+            }
+        }
+        T *o = stage + row_stage[t] + x;
+#pragma unroll
+        for (int c = 0; c < 3; c++) o[c * run] = from_float<T>(fmaf(v[c], g.scale[c], g.bias[c]));
+    }
+}
+
+template <typename T, bool kWide>
+__global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroups)) void patch_rows_tiled(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
                                                              const int32_t *__restrict__ status, T *__restrict__ out, int64_t out_stride,
                                                              int chunk)
 {
-    __shared__ alignas(16) uint8_t raw[kRawBytes];                      // the tile's source samples, rows 16-byte multiples apart
-    __shared__ alignas(16) float summed[kWaves][kSpan * 3 + 6];         // a row's samples summed over its window, of each wave
-    __shared__ alignas(16) T stage[stage_pixels((int)sizeof(T)) * 3];   // values by patch, channel, pixel
-    __shared__ alignas(16) float row_weight[kTileRows][kTaps];          // scaled to sum 1, then 0
-    __shared__ int32_t row_first[kTileRows], row_taps[kTileRows], row_stage[kTileRows];
-    __shared__ int32_t col_first[kTileCols], col_taps[kTileCols], col_stage[kTileCols];
+    typedef Limits<kWide, (int)sizeof(T)> Most;
+    constexpr int kSumPitch = Most::sum_pitch, kLoads = Most::loads;
+    __shared__ alignas(16) uint8_t raw[Most::raw_bytes + 64];    // (a product's last columns may lie behind the last row)
+    __shared__ alignas(16) float summed[kTileRows * kSumPitch];  // sums over rows, by output row and byte of a source row
+    __shared__ uint4 weight[Most::steps][2][64];                 // hi and lo as the product's lanes hold them
+    __shared__ int32_t row_first[kStrip * kTileRows], row_taps[kStrip * kTileRows], row_stage[kStrip * kTileRows];
+    __shared__ float row_centre[kStrip * kTileRows], row_norm[kStrip * kTileRows];
+    __shared__ int32_t col_first[kTileCols], col_taps[kTileCols], line_row[kStrip * kTileRows], column_row[kTileCols];
     __shared__ float col_centre[kTileCols], col_norm[kTileCols];
-    __shared__ int32_t patch_row[kPatches];
+    __shared__ int32_t patch_row[2][kPatches], tile_down[kStrip], tile_part_rows[kStrip], tile_part_y0[kStrip];
+    T *stage = reinterpret_cast<T *>(raw);  // values by patch, channel, pixel
 
     const int clip = clip_of(pack, blockIdx.x);
     const PatchClip &C = pack.c[clip];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t tile = blockIdx.x - pack.block0[clip];
-    const int frames_group = (int)(tile / (uint32_t)(C.tiles_x * C.tiles_y));
-    tile -= (uint32_t)frames_group * (uint32_t)(C.tiles_x * C.tiles_y);
-    const int tile_y = (int)(tile / (uint32_t)C.tiles_x), tile_x = (int)(tile - (uint32_t)tile_y * (uint32_t)C.tiles_x);
-    const int cols = C.out_w / g.patch, rows = C.out_h / g.patch;
-    // the tile's patches, and its rows of pixels
-    const int px0 = tile_x * C.across, across = min(C.across, cols - px0);
-    const int py0 = tile_y / C.parts * C.down, down = min(C.down, rows - py0);
-    const int part_y0 = tile_y % C.parts * C.part_rows;
-    const int part_rows = C.parts > 1 ? min(C.part_rows, g.patch - part_y0) : g.patch;
-    const int tile_w = across * g.patch, tile_h = down * part_rows, x0 = px0 * g.patch, y0 = py0 * g.patch + part_y0;
-    const int run = part_rows * g.patch;  // of a patch's channel
-    // the source samples under it; at least kNarrowest columns, so that a row holds a read of 16 bytes
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const uint32_t strip = blockIdx.x - pack.block0[clip], frames_group = C.strips.quotient(strip);
+    const uint32_t in_group = strip - frames_group * C.strips.d, strip_y = C.strips_x.quotient(in_group);
+    const int tile_x = (int)(in_group - strip_y * C.strips_x.d), tile_y0 = (int)strip_y * g.strip;
+    const int tiles = min(g.strip, C.tiles_y - tile_y0);
+    const int px0 = tile_x * C.across, across = min(C.across, C.cols - px0);  // patches
+    const int tile_w = across * g.patch, x0 = px0 * g.patch;
     const bool antialias = g.antialias != 0;
-    int c_end = make_taps(x0 + tile_w - 1, C.width, C.scale_x, antialias).end;
-    const int c0 = max(min(make_taps(x0, C.width, C.scale_x, antialias).first, C.width - kNarrowest), 0);
-    c_end = max(c_end, min(c0 + kNarrowest, C.width));
-    const int r0 = make_taps(y0, C.height, C.scale_y, antialias).first, r_end = make_taps(y0 + tile_h - 1, C.height, C.scale_y, antialias).end;
-    const int bytes = (c_end - c0) * 3, units = (bytes + 15) / 16, raw_pitch = units * 16;
-
-    for (int t = threadIdx.x; t < tile_h; t += kThreads) {
-        const Taps w = make_taps(y0 + t, C.height, C.scale_y, antialias);
-        const int taps = w.end - w.first;
-        float sum = 0.0f;
-        for (int k = 0; k < taps; k++) sum += w.weight(k);
-        for (int k = 0; k < taps; k++) row_weight[t][k] = w.weight(k) / sum;
-        if (taps & 1) row_weight[t][taps] = 0.0f;
-        row_first[t] = w.first - r0;
-        row_taps[t] = taps;
-        const int patch = t / part_rows;
-        row_stage[t] = patch * across * 3 * run + (t - patch * part_rows) * g.patch;
-    }
-    for (int t = (int)threadIdx.x - 64; t < tile_w; t += kThreads) {
-        if (t < 0) continue;
-        const Taps w = make_taps(x0 + t, C.width, C.scale_x, antialias);
-        float sum = 0.0f;
-        for (int k = 0; k < w.end - w.first; k++) sum += w.weight(k);
-        col_first[t] = (w.first - c0) * 3;
-        col_taps[t] = w.end - w.first;
-        col_centre[t] = w.centre;
-        col_norm[t] = 1.0f / sum;
-        const int patch = t / g.patch;
-        col_stage[t] = patch * 3 * run + (t - patch * g.patch);
-    }
-    for (int t = threadIdx.x; t < down * across; t += kThreads) {
-        const int a = t / across;
-        patch_row[t] = row_of_patch(py0 + a, px0 + t - a * across, cols, g.merge);
-    }
-    const bool ok = status == nullptr || status[C.image] == PREP_OK;
     const float inv_x = (float)(1.0 / (antialias && C.scale_x > 1.0 ? C.scale_x : 1.0));
-    const int distinct = min(g.group, C.frames - frames_group * g.group);  // the last frame stands in for the others
-    out += (C.row0 + (int64_t)frames_group * rows * cols) * out_stride + (int64_t)part_y0 * g.patch;
-    const int64_t area = (int64_t)g.patch * g.patch;
+    const float inv_y = (float)(1.0 / (antialias && C.scale_y > 1.0 ? C.scale_y : 1.0));
 
-    for (int f = 0; f < distinct; f++) {
-        const uint8_t *src = rgb + C.src_off + (uint64_t)(frames_group * g.group + f) * C.frame_stride + (uint64_t)r0 * C.pitch + (uint64_t)c0 * 3;
-        if (ok) {
-            const int total = (r_end - r0) * units;
-            for (int u0 = 0; u0 < total; u0 += kLoads * kThreads) {
-                uint4 v[kLoads];
-#pragma unroll
-                for (int k = 0; k < kLoads; k++) {
-                    const int u = u0 + k * kThreads + (int)threadIdx.x;
-                    if (u < total) {
-                        const int r = u / units;
-                        v[k] = load_inside(src + (uint64_t)r * C.pitch, (u - r * units) * 16, bytes);
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < kLoads; k++) {
-                    const int u = u0 + k * kThreads + (int)threadIdx.x;
-                    if (u < total) *reinterpret_cast<uint4 *>(raw + u * 16) = v[k];
-                }
+    if (wave == 0) {
+        if (lane < tile_w) {
+            const Taps w = make_taps(x0 + lane, C.width, C.scale_x, antialias);
+            float sum = 0.0f;
+            for (int k = 0; k < w.end - w.first; k++) sum += w.weight(k);
+            col_first[lane] = w.first;
+            col_taps[lane] = w.end - w.first;
+            col_centre[lane] = w.centre;
+            col_norm[lane] = 1.0f / (sum * (kWeightScale * kBytePairScale));
+        }
+    } else if (wave == 1) {
+        // row t of tile i
+        const int i = lane / kTileRows, t = lane - i * kTileRows;
+        int line = tile_y0 + i, part = 0;
+        if (C.parts > 1) {
+            line = (tile_y0 + i) / C.parts;
+            part = tile_y0 + i - line * C.parts;
+        }
+        const int py0 = line * C.down, down = min(C.down, C.rows - py0), part_y0 = part * C.part_rows, part_rows = min(C.part_rows, g.patch - part_y0);
+        if (i < tiles) {
+            if (t < down) line_row[lane] = row_of_line(g, py0 + t, C.cols);
+            if (t < down * part_rows) {
+                const Taps w = make_taps(py0 * g.patch + part_y0 + t, C.height, C.scale_y, antialias);
+                float sum = 0.0f;
+                for (int k = 0; k < w.end - w.first; k++) sum += w.weight(k);
+                row_first[lane] = w.first;
+                row_taps[lane] = w.end - w.first;
+                row_centre[lane] = w.centre;
+                row_norm[lane] = kWeightScale / sum;
+                const int a = down == 1 ? 0 : (int)g.by_patch.quotient((uint32_t)t);  // (several lines of patches are whole ones)
+                row_stage[lane] = a * across * 3 * part_rows * g.patch + (t - a * part_rows) * g.patch;
+            }
+            if (t == 0) {
+                tile_down[i] = down;
+                tile_part_rows[i] = part_rows;
+                tile_part_y0[i] = part_y0;
             }
         }
-        __syncthreads();  // (the tables too)
-        for (int t = wave; t < tile_h; t += kWaves) {
-            if (ok) {
-                const uint8_t *first = raw + row_first[t] * raw_pitch;
-                const int taps = row_taps[t];
-                for (int at = lane * 8; at < bytes; at += 64 * 8) {
-                    float a[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                    const uint8_t *p = first + at;
-                    for (int k = 0; k < taps; k += 2) {
-                        // (an odd window's last row is read twice, the second time with weight 0)
-                        const uint2 v0 = *reinterpret_cast<const uint2 *>(p), v1 = *reinterpret_cast<const uint2 *>(k + 1 < taps ? p + raw_pitch : p);
-                        const float w0 = row_weight[t][k], w1 = row_weight[t][k + 1];
-                        p += 2 * raw_pitch;
+    } else if (wave == 2) {
+        if (lane < across) column_row[lane] = row_of_column(g, px0 + lane);
+    }
+    __syncthreads();
+    // the samples under the strip's columns; at least kNarrowest columns, so that a row holds a read of 16 bytes
+    const int c0 = uniform(max(min(col_first[0], C.width - kNarrowest), 0));
+    const int c_end = uniform(max(col_first[tile_w - 1] + col_taps[tile_w - 1], min(c0 + kNarrowest, C.width)));
+    const int bytes = (c_end - c0) * 3, units = (bytes + 15) / 16, raw_pitch = units * 16;
+    const bool ok = status == nullptr || status[C.image] == PREP_OK;
+    const int distinct = min(g.group, C.frames - (int)frames_group * g.group);  // the last frame stands in for the others
+    const uint8_t *src = rgb + C.src_off + (uint64_t)frames_group * (uint64_t)g.group * C.frame_stride + (uint64_t)c0 * 3;
+    out += (C.row0 + (int64_t)frames_group * C.rows * C.cols) * out_stride;
+    const int area = g.patch * g.patch;
+    const int groups = (bytes + 63) / 64;
+    // the thread's reads of a frame: row and column of each
+    int read_row[kLoads], read_at[kLoads];
+    uint4 read[kLoads];
 #pragma unroll
-                        for (int i = 0; i < 8; i++) {
-                            const uint32_t b0 = i < 4 ? v0.x : v0.y, b1 = i < 4 ? v1.x : v1.y;
-                            a[i] = fmaf(w0, (float)(b0 >> (8 * (i & 3)) & 255u), fmaf(w1, (float)(b1 >> (8 * (i & 3)) & 255u), a[i]));
+    for (int k = 0; k < kLoads; k++) {
+        const int u = k * kThreads + (int)threadIdx.x;
+        read_row[k] = u / units;
+        read_at[k] = (u - read_row[k] * units) * 16;
+    }
+
+    // Tile i, frame f is worked on while the frame after it is read; before the first, nothing is.
+    int i = 0, f = -1, n_rows = 0, down = 0, part_rows = 0, part_y0 = 0;
+    for (;;) {
+        if (f >= 0) {
+            if (ok) {
+#pragma unroll
+                for (int k = 0; k < kLoads; k++) {
+                    const int u = k * kThreads + (int)threadIdx.x;
+                    if (u < n_rows * units) *reinterpret_cast<uint4 *>(raw + u * 16) = moved_back(read[k], max(read_at[k] - (bytes - 16), 0));
+                }
+            }
+            __syncthreads();
+            if (ok) {
+                // sums over rows: a wave takes 64 bytes of all rows, four products of 16 (bytes 4 n + j)
+                for (int group = wave; group < groups; group += kWaves) {
+                    const int at = group * 64 + 4 * (lane & 15);
+                    float4 sum[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    for (int step = 0; step < Most::steps && 32 * step < n_rows; step++) {
+                        uint32_t b[8];
+#pragma unroll
+                        for (int j = 0; j < 8; j++) {
+                            const int k = min(32 * step + 4 * j + (lane >> 4), n_rows - 1);  // (weight 0 behind the last row)
+                            b[j] = *reinterpret_cast<const uint32_t *>(raw + k * raw_pitch + at);
+                        }
+                        const uint4 hi = weight[step][0][lane], lo = weight[step][1][lane];
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const uint4 column = make_uint4(byte_pair(b[0], b[1], j), byte_pair(b[2], b[3], j), byte_pair(b[4], b[5], j), byte_pair(b[6], b[7], j));
+                            sum[j] = multiply_add_16x16x32(lo, column, multiply_add_16x16x32(hi, column, sum[j]));
                         }
                     }
-                    float4 *s = reinterpret_cast<float4 *>(&summed[wave][at]);
-                    s[0] = make_float4(a[0], a[1], a[2], a[3]);
-                    s[1] = make_float4(a[4], a[5], a[6], a[7]);
+                    float *s = summed + 4 * (lane >> 4) * kSumPitch + at;
+                    *reinterpret_cast<float4 *>(s) = make_float4(sum[0].x, sum[1].x, sum[2].x, sum[3].x);
+                    *reinterpret_cast<float4 *>(s + kSumPitch) = make_float4(sum[0].y, sum[1].y, sum[2].y, sum[3].y);
+                    *reinterpret_cast<float4 *>(s + 2 * kSumPitch) = make_float4(sum[0].z, sum[1].z, sum[2].z, sum[3].z);
+                    *reinterpret_cast<float4 *>(s + 3 * kSumPitch) = make_float4(sum[0].w, sum[1].w, sum[2].w, sum[3].w);
                 }
-                wave_sync();
             }
-            for (int x = lane; x < tile_w; x += 64) {
-                float v[3] = {0.0f, 0.0f, 0.0f};
-                if (ok) {
-                    const float *s = &summed[wave][col_first[x]];
-                    const float centre = col_centre[x], norm = col_norm[x];
-                    const int taps = col_taps[x];
-                    for (int k = 0; k < taps; k++) {
-                        const float w = fmaxf(0.0f, fmaf(-fabsf((float)k - centre), inv_x, 1.0f));
+            __syncthreads();
+        }
+        // what comes next
+        const int i_next = f + 1 == distinct ? i + 1 : i, f_next = f + 1 == distinct ? 0 : f + 1;
+        const bool more = i_next < tiles;
+        int n_next = n_rows, down_next = down, part_rows_next = part_rows, part_y0_next = part_y0;
+        if (more) {
+            const int row = i_next * kTileRows, r0 = uniform(row_first[row]);
+            if (f_next == 0) {
+                down_next = uniform(tile_down[i_next]);
+                part_rows_next = uniform(tile_part_rows[i_next]);
+                part_y0_next = uniform(tile_part_y0[i_next]);
+                const int end = row + down_next * part_rows_next - 1;
+                n_next = uniform(row_first[end] + row_taps[end]) - r0;
+            }
+            if (ok) {
+                // (all reads go out before the first is waited for)
+                const uint8_t *frame = src + (uint64_t)f_next * C.frame_stride + (uint64_t)(uint32_t)r0 * C.pitch;
 #pragma unroll
-                        for (int c = 0; c < 3; c++) v[c] = fmaf(w, s[3 * k + c], v[c]);
+                for (int k = 0; k < kLoads; k++)
+                    if (k * kThreads < n_next * units)
+                        __builtin_memcpy(&read[k], frame + (uint64_t)(uint32_t)min(read_row[k], n_next - 1) * C.pitch + min(read_at[k], bytes - 16), 16);
+            }
+            if (f_next == 0) {
+                // Weights for 32 source rows a wave: lane l of a product holds rows 4 j + l / 16, j = 0 .. 7.
+                const int m = lane & 15;
+                if (32 * wave < n_next) {
+                    uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+                    if (m < down_next * part_rows_next) {
+                        const int begin = row_first[row + m] - r0 - 32 * wave - (lane >> 4), n = row_taps[row + m];
+                        const float centre = row_centre[row + m], scale = row_norm[row + m];
+#pragma unroll
+                        for (int j = 0; j < 8; j++) {
+                            const int tap = 4 * j - begin;
+                            const float w = tap >= 0 && tap < n ? fmaxf(0.0f, fmaf(-fabsf((float)tap - centre), inv_y, 1.0f)) * scale : 0.0f;
+                            const __half h = __float2half_rn(w);
+                            const __half r = __float2half_rn(w - __half2float(h));
+                            uint16_t hb, rb;
+                            __builtin_memcpy(&hb, &h, 2);
+                            __builtin_memcpy(&rb, &r, 2);
+                            hi[j >> 1] |= (uint32_t)hb << (16 * (j & 1));
+                            lo[j >> 1] |= (uint32_t)rb << (16 * (j & 1));
+                        }
                     }
-#pragma unroll
-                    for (int c = 0; c < 3; c++) v[c] = fmaf(v[c] * norm, g.scale[c], g.bias[c]);
+                    weight[wave][0][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    weight[wave][1][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 }
-                T *o = stage + row_stage[t] + col_stage[x];
-#pragma unroll
-                for (int c = 0; c < 3; c++) o[c * run] = from_float<T>(v[c]);
+                for (int p = threadIdx.x; p < down_next * across; p += kThreads) {
+                    const int a = down_next == 1 ? 0 : p / across;
+                    patch_row[i_next & 1][p] = line_row[row + a] + column_row[p - a * across];
+                }
             }
-            if (ok) wave_sync();
         }
-        __syncthreads();
-        for (int slot = f; slot < (f + 1 == distinct ? g.group : f + 1); slot++) {
-            T *o = out + slot * area;
-            const int64_t channel = g.group * area;
-            if (chunk == 16) write_runs<T, 16>(stage, patch_row, down * across * 3, run, o, out_stride, channel);
-            else if (chunk == 8) write_runs<T, 8>(stage, patch_row, down * across * 3, run, o, out_stride, channel);
-            else if (chunk == 4) write_runs<T, 4>(stage, patch_row, down * across * 3, run, o, out_stride, channel);
-            else write_runs<T, (int)sizeof(T)>(stage, patch_row, down * across * 3, run, o, out_stride, channel);
+        if (f >= 0) {
+            const int run = part_rows * g.patch, tile_h = down * part_rows;  // of a patch's channel
+            if (ok) {
+                if (lane < tile_w) {
+                    const int patch = (int)g.by_patch.quotient((uint32_t)lane), x_stage = patch * 3 * run + (lane - patch * g.patch);
+                    const int first = col_first[lane] - c0, taps = col_taps[lane], most = groups * 64 / 3;
+                    const float centre = col_centre[lane], norm = col_norm[lane];
+                    const int32_t *rows = row_stage + i * kTileRows;
+                    if (!kWide)
+                        sum_columns<T, kFewTaps, kSumPitch>(summed, stage, rows, tile_h, x_stage, first, taps, centre, inv_x, norm, most, run, g);
+                    else if (columns_of_window(C.scale_x, antialias) <= kSomeTaps)
+                        sum_columns<T, kSomeTaps, kSumPitch>(summed, stage, rows, tile_h, x_stage, first, taps, centre, inv_x, norm, most, run, g);
+                    else
+                        sum_columns<T, 0, kSumPitch>(summed, stage, rows, tile_h, x_stage, first, taps, centre, inv_x, norm, most, run, g);
+                }
+            } else {
+                for (int e = threadIdx.x; e < tile_w * tile_h * 3; e += kThreads) stage[e] = from_float<T>(0.0f);
+            }
+            __syncthreads();
+            for (int slot = f; slot < (f + 1 == distinct ? g.group : f + 1); slot++) {
+                T *o = out + slot * area + part_y0 * g.patch;
+                const int channel = g.group * area;
+                if (chunk == 16) write_runs<T, 16>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
+                else if (chunk == 8) write_runs<T, 8>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
+                else if (chunk == 4) write_runs<T, 4>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
+                else write_runs<T, (int)sizeof(T)>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
+            }
+            __syncthreads();
         }
-        // (raw is not read any more, and the barrier before the next frame's sums ends the stage's reads)
+        if (!more) break;
+        i = i_next;
+        f = f_next;
+        n_rows = n_next;
+        down = down_next;
+        part_rows = part_rows_next;
+        part_y0 = part_y0_next;
     }
 }
 
@@ -307,8 +444,8 @@ __global__ __launch_bounds__(kThreads) void patch_rows_direct(const uint8_t *__r
     const int clip = clip_of(pack, blockIdx.x);
     const PatchClip &C = pack.c[clip];
     const int area = g.patch * g.patch;
-    const int cols = C.out_w / g.patch, rows = C.out_h / g.patch;
-    const int64_t per_frame = (int64_t)C.out_w * C.out_h;
+    const int cols = C.cols, rows = C.rows;
+    const int64_t per_frame = (int64_t)cols * rows * area;
     const int64_t item = (int64_t)(blockIdx.x - pack.block0[clip]) * kThreads + threadIdx.x;
     const int groups = (C.frames - 1) / g.group + 1;
     if (item >= per_frame * g.group * groups) return;
@@ -399,19 +536,18 @@ bool patch_size(const prep_patch_params *p, int32_t width, int32_t height, int32
     return true;
 }
 
-// How a clip is cut into tiles; false = it is not (see patch_rows_direct).
-bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int element)
+// How a clip is cut into tiles, one way or the other; false = it is not.
+template <typename Most>
+bool cut_into_tiles(PatchClip *c, const PatchGeometry &g)
 {
     if (c->width < kNarrowest) return false;
     const double sx = g.antialias && c->scale_x > 1.0 ? c->scale_x : 1.0, sy = g.antialias && c->scale_y > 1.0 ? c->scale_y : 1.0;
-    if (2.0 * sy + 2.0 > (double)kTaps) return false;
-    const int cols = c->out_w / g.patch, rows = c->out_h / g.patch;
-    // the most source columns and rows under `n` output samples in a row
-    auto span = [](int n, double scale, double s) { return (n - 1) * scale + 2.0 * s + 2.0; };
     auto fits = [&](int across, int tall) {
+        // at most so many source columns and rows lie under that many output samples in a row
         const int w = across * g.patch;
-        const double x = fmax(span(w, c->scale_x, sx), (double)kNarrowest), y = span(tall, c->scale_y, sy);
-        return w <= kTileCols && tall <= kTileRows && w * tall <= stage_pixels(element) && x <= (double)kSpan && y * (3.0 * x + 16.0) <= (double)kRawBytes;
+        const double x = fmax((w - 1) * c->scale_x + 2.0 * sx + 2.0, (double)kNarrowest), y = (tall - 1) * c->scale_y + 2.0 * sy + 2.0;
+        return w <= kTileCols && tall <= kTileRows && 3.0 * x <= (double)Most::span_bytes && y <= (double)Most::source_rows &&
+               y * (3.0 * x + 16.0) <= (double)Most::raw_bytes;
     };
     c->parts = 1;
     c->part_rows = g.patch;
@@ -422,19 +558,35 @@ bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int element)
     }
     c->parts = (g.patch + c->part_rows - 1) / c->part_rows;
     c->across = c->down = 1;
-    while (c->across < cols && fits(c->across + 1, c->part_rows)) c->across++;
+    while (c->across < c->cols && fits(c->across + 1, c->part_rows)) c->across++;
     if (c->parts == 1)
-        while (c->down < rows && (c->down + 1) * c->across <= kPatches && fits(c->across, (c->down + 1) * g.patch)) c->down++;
-    c->tiles_x = (cols + c->across - 1) / c->across;
-    c->tiles_y = (rows + c->down - 1) / c->down * c->parts;
+        while (c->down < c->rows && (c->down + 1) * c->across <= kPatches && fits(c->across, (c->down + 1) * g.patch)) c->down++;
+    c->tiles_x = (c->cols + c->across - 1) / c->across;
+    c->tiles_y = (c->rows + c->down - 1) / c->down * c->parts;
     return true;
 }
 
-uint64_t blocks_of(const PatchClip &c, const PatchGeometry &g, bool tiled)
+// The kernels: patch_rows_direct, patch_rows_tiled with kWide = false and true.
+enum { kDirect = 0, kNarrow = 1, kWide = 2, kKinds = 3 };
+
+template <int kElement>
+int kind_of(PatchClip *c, const PatchGeometry &g)
 {
-    const uint64_t groups = (uint64_t)((c.frames - 1) / g.group + 1);
-    if (tiled) return groups * (uint64_t)c.tiles_x * (uint64_t)c.tiles_y;
-    return ((uint64_t)c.out_w * (uint64_t)c.out_h * groups * (uint64_t)g.group + kThreads - 1) / kThreads;
+    // The narrow kind keeps five workgroups on a compute unit where the wide one keeps three; what is reduced so far that its tiles
+    // would be narrower than the other's is the wide kind's.
+    PatchClip wide = *c;
+    const bool fits_wide = cut_into_tiles<Limits<true, kElement>>(&wide, g);
+    if (columns_of_window(c->scale_x, g.antialias) <= kFewTaps && cut_into_tiles<Limits<false, kElement>>(c, g) && (!fits_wide || c->across * c->down * c->part_rows >= wide.across * wide.down * wide.part_rows))
+        return kNarrow;
+    *c = wide;
+    return fits_wide ? kWide : kDirect;
+}
+
+uint64_t groups_of(const PatchClip &c, const PatchGeometry &g) { return (uint64_t)((c.frames - 1) / g.group + 1); }
+uint64_t blocks_of(const PatchClip &c, const PatchGeometry &g, int kind)
+{
+    if (kind != kDirect) return groups_of(c, g) * c.strips.d;
+    return ((uint64_t)c.cols * (uint64_t)c.rows * (uint64_t)(g.patch * g.patch) * groups_of(c, g) * (uint64_t)g.group + kThreads - 1) / kThreads;
 }
 
 // Bytes that all runs can be written by at a time.
@@ -449,44 +601,58 @@ int chunk_bytes(const prep_patch_params *params, const ClipPack &pack, int n, co
 }
 
 template <typename T>
-void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, const PatchGeometry &g, bool tiled, int chunk, const int32_t *status,
+void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, const PatchGeometry &g, int kind, int chunk, const int32_t *status,
                 T *out, int64_t out_stride, hipStream_t stream)
 {
-    if (tiled)
-        hipLaunchKernelGGL((patch_rows_tiled<T>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
+    if (kind == kWide)
+        hipLaunchKernelGGL((patch_rows_tiled<T, true>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
+    else if (kind == kNarrow)
+        hipLaunchKernelGGL((patch_rows_tiled<T, false>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
     else
         hipLaunchKernelGGL((patch_rows_direct<T>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride);
 }
 
-// status: DEVICE, per PatchClip::image, or nullptr = all PREP_OK (others get rows of zeros).  clips: HOST, n of them, all but
-// the tiles filled in.  Every clip is taken by a launch of one kind or the other.
-int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, int32_t n, const prep_patch_params *params, const int32_t *status, void *out,
-                      int64_t out_stride, hipStream_t stream)
+// status: DEVICE, per PatchClip::image, or nullptr = all PREP_OK (others get rows of zeros).  clips, kinds: HOST, n of them; the tiles
+// and kinds are found here.  Every clip is taken by a launch of its kind.
+int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int32_t n, const prep_patch_params *params, const int32_t *status,
+                      void *out, int64_t out_stride, hipStream_t stream)
 {
     PatchGeometry g;
     g.patch = params->patch;
     g.merge = params->merge;
     g.group = params->frames_per_patch;
     g.antialias = params->filter == PREP_FILTER_ANTIALIAS;
+    g.by_patch = divisor(g.patch);
+    g.by_merge = divisor(g.merge);
     for (int c = 0; c < 3; c++) {
         g.scale[c] = (float)(1.0 / (255.0 * (double)params->std[c]));
         g.bias[c] = (float)(-(double)params->mean[c] / (double)params->std[c]);
     }
-    bool any[2] = {false, false};
+    bool any[kKinds] = {false, false, false};
+    uint64_t tiles = 0;
     for (int32_t i = 0; i < n; i++) {
-        if (!cut_into_tiles(&clips[i], g, element_bytes(params->out_dtype))) clips[i].tiles_x = 0;
-        any[clips[i].tiles_x != 0] = true;
+        PatchClip &c = clips[i];
+        kinds[i] = (uint8_t)(element_bytes(params->out_dtype) == 2 ? kind_of<2>(&c, g) : kind_of<4>(&c, g));
+        any[kinds[i]] = true;
+        if (kinds[i] != kDirect) tiles += groups_of(c, g) * (uint64_t)c.tiles_x * (uint64_t)c.tiles_y;
     }
-    for (int kind = 0; kind < 2; kind++) {
-        const bool tiled = kind == 1;
+    // a workgroup takes a strip of tiles where there are plenty, so that it can read one while it works on another
+    g.strip = (int)(tiles / 1536 < 1 ? 1 : tiles / 1536 > kStrip ? kStrip : tiles / 1536);
+    for (int32_t i = 0; i < n; i++) {
+        PatchClip &c = clips[i];
+        if (kinds[i] == kDirect) continue;
+        c.strips_x = divisor(c.tiles_x);
+        c.strips = divisor(c.tiles_x * ((c.tiles_y + g.strip - 1) / g.strip));
+    }
+    for (int kind = 0; kind < kKinds; kind++) {
         if (!any[kind]) continue;
         for (int32_t at = 0; at < n;) {
             ClipPack pack;
             uint64_t blocks = 0;
             int m = 0;
             for (; at < n && m < kClips; at++) {
-                if ((clips[at].tiles_x != 0) != tiled) continue;
-                const uint64_t mine = blocks_of(clips[at], g, tiled);
+                if (kinds[at] != kind) continue;
+                const uint64_t mine = blocks_of(clips[at], g, kind);
                 if (blocks + mine > 0x7FFFFFFFull) break;
                 pack.c[m] = clips[at];
                 pack.block0[m] = (uint32_t)blocks;
@@ -498,13 +664,13 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, int32_t n, const pre
                 pack.c[k] = pack.c[0];
                 pack.block0[k] = 0xFFFFFFFFu;
             }
-            const int chunk = tiled ? chunk_bytes(params, pack, m, out, out_stride) : 0;
+            const int chunk = kind != kDirect ? chunk_bytes(params, pack, m, out, out_stride) : 0;
             if (params->out_dtype == PREP_F16)
-                launch_for(rgb, pack, (uint32_t)blocks, g, tiled, chunk, status, (__half *)out, out_stride, stream);
+                launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (__half *)out, out_stride, stream);
             else if (params->out_dtype == PREP_BF16)
-                launch_for(rgb, pack, (uint32_t)blocks, g, tiled, chunk, status, (__hip_bfloat16 *)out, out_stride, stream);
+                launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (__hip_bfloat16 *)out, out_stride, stream);
             else
-                launch_for(rgb, pack, (uint32_t)blocks, g, tiled, chunk, status, (float *)out, out_stride, stream);
+                launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (float *)out, out_stride, stream);
         }
     }
     return PREP_OK;
@@ -517,7 +683,11 @@ public:
         : params_(params), out_(out), out_stride_(out_stride), out_rows_(out_rows), row_starts_(row_starts), n_(n)
     {
     }
-    ~PatchCall() { delete[] clips_; }
+    ~PatchCall()
+    {
+        delete[] clips_;
+        delete[] kinds_;
+    }
     PatchCall(const PatchCall &) = delete;
     PatchCall &operator=(const PatchCall &) = delete;
 
@@ -528,7 +698,7 @@ public:
         if (out_stride_ == 0) out_stride_ = row;
         if (out_stride_ < row || !aligned(out_, (uintptr_t)element_bytes(params_->out_dtype))) return PREP_E_INVALID_ARG;
         row_starts_[0] = 0;
-        if (n_ > 0 && !(clips_ = new (std::nothrow) PatchClip[(size_t)n_])) return PREP_E_NOMEM;
+        if (n_ > 0 && (!(clips_ = new (std::nothrow) PatchClip[(size_t)n_]) || !(kinds_ = new (std::nothrow) uint8_t[(size_t)n_]))) return PREP_E_NOMEM;
         return PREP_OK;
     }
     // Clips come in ascending order; those left out have no rows.
@@ -547,10 +717,10 @@ public:
         c.pitch = pitch;
         c.width = width;
         c.height = height;
-        c.out_w = cols * params_->patch;
-        c.out_h = rows * params_->patch;
-        c.scale_x = (double)width / (double)c.out_w;
-        c.scale_y = (double)height / (double)c.out_h;
+        c.cols = cols;
+        c.rows = rows;
+        c.scale_x = (double)width / (double)(cols * params_->patch);
+        c.scale_y = (double)height / (double)(rows * params_->patch);
         c.frames = frames;
         c.image = i;
         row_starts_[i + 1] = row_starts_[i] + groups * rows * cols;
@@ -564,7 +734,7 @@ public:
     }
     int launch(const uint8_t *rgb, const int32_t *status, hipStream_t stream)
     {
-        return launch_patch_rows(rgb, clips_, count_, params_, status, out_, out_stride_, stream);
+        return launch_patch_rows(rgb, clips_, kinds_, count_, params_, status, out_, out_stride_, stream);
     }
 
 private:
@@ -577,6 +747,7 @@ private:
     int64_t out_stride_, out_rows_, *row_starts_;
     int32_t n_, count_ = 0, next_ = 0;
     PatchClip *clips_ = nullptr;
+    uint8_t *kinds_ = nullptr;
 };
 
 // Behind the JPEG decoder.

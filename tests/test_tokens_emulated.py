@@ -16,7 +16,7 @@ SOURCES = emul.KERNELS + [k for k in ("patches.hip", "packing.hip", "rotary.hip"
 
 def build():
     srcs = [os.path.join(emul.CSRC, k) for k in SOURCES] + [os.path.join(emul.EMU, "emul_runtime.cpp")]
-    deps = srcs + [os.path.join(emul.CSRC, x) for x in ("kernels.h", "parser.h", "prep_internal.h", "tokens.h")] + \
+    deps = srcs + [os.path.join(emul.CSRC, x) for x in ("kernels.h", "parser.h", "prep_internal.h", "tokens.h", "matrix.h")] + \
         [os.path.join(emul.ROOT, "include", "prep.h"), os.path.join(emul.EMU, "more_hip.h")] + [os.path.join(emul.EMU, "hip", x) for x in os.listdir(os.path.join(emul.EMU, "hip"))]
     if os.path.exists(LIBRARY) and os.path.getmtime(LIBRARY) >= max(os.path.getmtime(d) for d in deps):
         return
