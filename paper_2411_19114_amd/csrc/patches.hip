@@ -25,7 +25,7 @@ namespace prep {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256;
 constexpr int kClips = 32;  // clips of one launch: their records are kernel arguments (3 KB), so that a call has
                             // no workspace, calls may overlap and a captured call keeps its own
 
@@ -50,11 +50,10 @@ template <bool kWide, int kElement>
 struct Limits {
     static constexpr int span_bytes = kWide ? 448 : 256, sum_pitch = span_bytes + 4;  // of a source row
     static constexpr int steps = kWide ? 2 : 1, source_rows = 32 * steps;  // products over 32 source rows each
-    // source samples, rows 16-byte multiples apart; the values for the patch rows afterwards
-    static constexpr int raw_bytes = kWide ? 16 << 10 : kElement == 2 ? 8 << 10 : 12 << 10;
-    static constexpr int loads = raw_bytes / (16 * kThreads);  // 16-byte reads of a thread
-    static constexpr int workgroups = kWide ? 3 : kElement == 2 ? 5 : 4;  // that a compute unit's LDS holds
-    static_assert(kTileCols * kTileRows * 3 * kElement <= raw_bytes, "the values take the samples' place");
+    static constexpr int raw_bytes = kWide ? 16 << 10 : 8 << 10;           // source samples, rows 16-byte multiples apart
+    static constexpr int threads = kWide ? 512 : 256, waves = threads / 64;
+    static constexpr int loads = raw_bytes / (16 * threads);               // 16-byte reads of a thread
+    static constexpr int workgroups = kWide ? 2 : kElement == 2 ? 4 : 3;   // that a compute unit's LDS holds
 };
 
 // One clip as the kernels see it.
@@ -64,14 +63,16 @@ struct PatchClip {
     int64_t row0;           // its first row
     double scale_x, scale_y;  // source samples per output sample
     uint32_t pitch;
-    int32_t width, height;  // pixels
-    int32_t cols, rows;     // patches
+    uint16_t width, height; // pixels
+    uint16_t cols, rows;    // patches
     int32_t frames;
     int32_t image;          // index into `status`
     // tiles: patches across and down, rows of a patch in it (fewer than the patch has where that is tall: `parts` tiles
     // share a patch then), tiles across and down; strips of tiles across and down
-    int32_t across, down, part_rows, parts, tiles_x, tiles_y;
+    uint16_t across, down, part_rows, parts;
+    int32_t tiles_x, tiles_y;
     Divisor strips_x, strips;  // in a row of them; of a frame group
+    Divisor chunks, last_chunks;  // written at a time, of a patch's channel in a tile; in the last tile of a patch
 };
 struct ClipPack {
     uint32_t block0[kClips];  // first workgroup of each clip; of those that the launch lacks 2^32 - 1
@@ -156,43 +157,42 @@ template <> struct Chunk<8> { typedef uint2 type; };
 template <> struct Chunk<4> { typedef uint32_t type; };
 template <> struct Chunk<2> { typedef uint16_t type; };
 
-// A frame's runs of `run` elements, `n` of them (three of a patch), from the stage to the patches' rows, kBytes at a time.
-template <typename T, int kBytes>
-__device__ __forceinline__ void write_runs(const T *stage, const int32_t *row, int n, int run, T *out, int64_t out_stride, int channel_stride)
+// A frame's runs, `n` of them (three of a patch), from the stage to the patches' rows, kBytes at a time; of `chunks` each.  Offsets from
+// `out` stay below 2^31 elements (see cut_into_tiles).
+template <typename T, int kBytes, int kThreads>
+__device__ __forceinline__ void write_runs(const T *stage, const int32_t *row, int n, const Divisor &chunks, T *out, int stride, int channel_stride)
 {
     typedef typename Chunk<kBytes>::type C;
     constexpr int kElements = kBytes / (int)sizeof(T);
-    const int chunks = run / kElements, by = kThreads / chunks, rest = kThreads - by * chunks;
-    int r = (int)threadIdx.x / chunks, at = (int)threadIdx.x - r * chunks;
-    while (r < n) {
-        const int patch = r / 3, channel = r - 3 * patch;
-        T *o = out + row[patch] * out_stride + channel * channel_stride + at * kElements;
-        *reinterpret_cast<C *>(o) = *reinterpret_cast<const C *>(stage + r * run + at * kElements);
-        r += by;
-        at += rest;
-        if (at >= chunks) {
-            at -= chunks;
-            r++;
-        }
+    for (uint32_t u = threadIdx.x; u < (uint32_t)n * chunks.d; u += kThreads) {
+        const uint32_t r = chunks.quotient(u), patch = r / 3, channel = r - 3 * patch;
+        const int at = row[patch] * stride + (int)(channel * (uint32_t)channel_stride + (u - r * chunks.d) * kElements);
+        *reinterpret_cast<C *>(out + at) = *reinterpret_cast<const C *>(stage + u * kElements);
     }
 }
 
-// Sums over the columns of a lane's window, kTaps samples wide, weights in registers; kTaps = 0: any width, weights formed again for each row.
-template <typename T, int kTaps, int kSumPitch>
-__device__ __forceinline__ void sum_columns(const float *summed, T *stage, const int32_t *row_stage, int tile_h, int x, int first, int taps, float centre,
-                                            float inv, float norm, int most, int run, const PatchGeometry &g)
-{
-    // a window starts earlier where kTaps samples would end behind the row's sums; what is not under the triangle has weight 0
-    const int at = kTaps != 0 ? min(first, most - kTaps) : first;
+// A lane's output column: its window in the row's sums, kTaps samples wide, and their weights; kTaps = 0: any width, weights formed for
+// every row.
+template <int kTaps>
+struct Column {
+    int at;      // first sample
+    int taps;    // kTaps = 0
+    float centre, inv, norm;
     float w[kTaps != 0 ? kTaps : 1];
+    // a window starts earlier where kTaps samples would end behind the row's sums; what is not under the triangle has weight 0
+    __device__ __forceinline__ Column(int first, int taps_, float centre_, float inv_, float norm_, int most)
+        : at(kTaps != 0 ? min(first, most - kTaps) : first), taps(taps_), centre(centre_), inv(inv_), norm(norm_)
+    {
 #pragma unroll
-    for (int k = 0; k < kTaps; k++) {
-        const int tap = at + k - first;
-        w[k] = tap >= 0 && tap < taps ? fmaxf(0.0f, fmaf(-fabsf((float)tap - centre), inv, 1.0f)) * norm : 0.0f;
+        for (int k = 0; k < kTaps; k++) {
+            const int tap = at + k - first;
+            w[k] = tap >= 0 && tap < taps ? fmaxf(0.0f, fmaf(-fabsf((float)tap - centre), inv, 1.0f)) * norm : 0.0f;
+        }
     }
-    for (int t = (int)threadIdx.x >> 6; t < tile_h; t += kWaves) {
-        const float *s = summed + t * kSumPitch + at * 3;
-        float v[3] = {0.0f, 0.0f, 0.0f};
+    __device__ __forceinline__ void sum(const float *summed, float v[3]) const
+    {
+        const float *s = summed + at * 3;
+        v[0] = v[1] = v[2] = 0.0f;
         if (kTaps != 0) {
 #pragma unroll
             for (int k = 0; k < kTaps; k++)
@@ -205,28 +205,37 @@ __device__ __forceinline__ void sum_columns(const float *summed, T *stage, const
                 for (int c = 0; c < 3; c++) v[c] = fmaf(wk, s[3 * k + c], v[c]);
             }
         }
-        T *o = stage + row_stage[t] + x;
+    }
+};
+template <typename T, int kTaps, int kSumPitch, int kWaves>
+__device__ __forceinline__ void sum_columns(const Column<kTaps> &column, const float *summed, T *stage, const int32_t *row_stage, int tile_h, int x_stage,
+                                            int run, const PatchGeometry &g)
+{
+    for (int t = uniform((int)threadIdx.x >> 6); t < tile_h; t += kWaves) {
+        float v[3];
+        column.sum(summed + t * kSumPitch, v);
+        T *o = stage + uniform(row_stage[t]) + x_stage;
 #pragma unroll
         for (int c = 0; c < 3; c++) o[c * run] = from_float<T>(fmaf(v[c], g.scale[c], g.bias[c]));
     }
 }
 
 template <typename T, bool kWide>
-__global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroups)) void patch_rows_tiled(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
+__global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<kWide, (int)sizeof(T)>::waves / 4 * Limits<kWide, (int)sizeof(T)>::workgroups)) void patch_rows_tiled(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
                                                              const int32_t *__restrict__ status, T *__restrict__ out, int64_t out_stride,
                                                              int chunk)
 {
     typedef Limits<kWide, (int)sizeof(T)> Most;
-    constexpr int kSumPitch = Most::sum_pitch, kLoads = Most::loads;
+    constexpr int kSumPitch = Most::sum_pitch, kLoads = Most::loads, kThreads = Most::threads, kWaves = Most::waves;
     __shared__ alignas(16) uint8_t raw[Most::raw_bytes + 64];    // (a product's last columns may lie behind the last row)
     __shared__ alignas(16) float summed[kTileRows * kSumPitch];  // sums over rows, by output row and byte of a source row
+    __shared__ alignas(16) T stage[kTileRows * kTileCols * 3];   // values by patch, channel, pixel
     __shared__ uint4 weight[Most::steps][2][64];                 // hi and lo as the product's lanes hold them
     __shared__ int32_t row_first[kStrip * kTileRows], row_taps[kStrip * kTileRows], row_stage[kStrip * kTileRows];
     __shared__ float row_centre[kStrip * kTileRows], row_norm[kStrip * kTileRows];
     __shared__ int32_t col_first[kTileCols], col_taps[kTileCols], line_row[kStrip * kTileRows], column_row[kTileCols];
     __shared__ float col_centre[kTileCols], col_norm[kTileCols];
     __shared__ int32_t patch_row[2][kPatches], tile_down[kStrip], tile_part_rows[kStrip], tile_part_y0[kStrip];
-    T *stage = reinterpret_cast<T *>(raw);  // values by patch, channel, pixel
 
     const int clip = clip_of(pack, blockIdx.x);
     const PatchClip &C = pack.c[clip];
@@ -235,7 +244,7 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
     const uint32_t in_group = strip - frames_group * C.strips.d, strip_y = C.strips_x.quotient(in_group);
     const int tile_x = (int)(in_group - strip_y * C.strips_x.d), tile_y0 = (int)strip_y * g.strip;
     const int tiles = min(g.strip, C.tiles_y - tile_y0);
-    const int px0 = tile_x * C.across, across = min(C.across, C.cols - px0);  // patches
+    const int px0 = tile_x * C.across, across = min((int)C.across, C.cols - px0);  // patches
     const int tile_w = across * g.patch, x0 = px0 * g.patch;
     const bool antialias = g.antialias != 0;
     const float inv_x = (float)(1.0 / (antialias && C.scale_x > 1.0 ? C.scale_x : 1.0));
@@ -259,7 +268,7 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
             line = (tile_y0 + i) / C.parts;
             part = tile_y0 + i - line * C.parts;
         }
-        const int py0 = line * C.down, down = min(C.down, C.rows - py0), part_y0 = part * C.part_rows, part_rows = min(C.part_rows, g.patch - part_y0);
+        const int py0 = line * C.down, down = min((int)C.down, C.rows - py0), part_y0 = part * C.part_rows, part_rows = min((int)C.part_rows, g.patch - part_y0);
         if (i < tiles) {
             if (t < down) line_row[lane] = row_of_line(g, py0 + t, C.cols);
             if (t < down * part_rows) {
@@ -283,10 +292,11 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
         if (lane < across) column_row[lane] = row_of_column(g, px0 + lane);
     }
     __syncthreads();
-    // the samples under the strip's columns; at least kNarrowest columns, so that a row holds a read of 16 bytes
-    const int c0 = uniform(max(min(col_first[0], C.width - kNarrowest), 0));
-    const int c_end = uniform(max(col_first[tile_w - 1] + col_taps[tile_w - 1], min(c0 + kNarrowest, C.width)));
-    const int bytes = (c_end - c0) * 3, units = (bytes + 15) / 16, raw_pitch = units * 16;
+    // the samples under the strip's columns, in sixteens (48 bytes, whole reads of 16) unless the image is narrower
+    const int c_end = uniform(col_first[tile_w - 1] + col_taps[tile_w - 1]), sixteens = (c_end - uniform(col_first[0]) + 15) / 16;
+    const int span = min(16 * sixteens, (int)C.width), c0 = min(uniform(col_first[0]), C.width - span);
+    const int bytes = span * 3, units = (bytes + 15) / 16, raw_pitch = units * 16;
+    const bool whole = span == 16 * sixteens;
     const bool ok = status == nullptr || status[C.image] == PREP_OK;
     const int distinct = min(g.group, C.frames - (int)frames_group * g.group);  // the last frame stands in for the others
     const uint8_t *src = rgb + C.src_off + (uint64_t)frames_group * (uint64_t)g.group * C.frame_stride + (uint64_t)c0 * 3;
@@ -303,18 +313,16 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
         read_at[k] = (u - read_row[k] * units) * 16;
     }
 
+    // the lane's output column
+    constexpr int kColumnTaps = kWide ? kSomeTaps : kFewTaps;
+    const int x = min(lane, tile_w - 1), patch = (int)g.by_patch.quotient((uint32_t)x);
+    const bool any_taps = kWide && columns_of_window(C.scale_x, antialias) > kSomeTaps;
+    const Column<kColumnTaps> column(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], groups * 64 / 3);
+
     // Tile i, frame f is worked on while the frame after it is read; before the first, nothing is.
     int i = 0, f = -1, n_rows = 0, down = 0, part_rows = 0, part_y0 = 0;
     for (;;) {
         if (f >= 0) {
-            if (ok) {
-#pragma unroll
-                for (int k = 0; k < kLoads; k++) {
-                    const int u = k * kThreads + (int)threadIdx.x;
-                    if (u < n_rows * units) *reinterpret_cast<uint4 *>(raw + u * 16) = moved_back(read[k], max(read_at[k] - (bytes - 16), 0));
-                }
-            }
-            __syncthreads();
             if (ok) {
                 // sums over rows: a wave takes 64 bytes of all rows, four products of 16 (bytes 4 n + j)
                 for (int group = wave; group < groups; group += kWaves) {
@@ -322,6 +330,7 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
                     float4 sum[4];
 #pragma unroll
                     for (int j = 0; j < 4; j++) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
                     for (int step = 0; step < Most::steps && 32 * step < n_rows; step++) {
                         uint32_t b[8];
 #pragma unroll
@@ -364,7 +373,7 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
 #pragma unroll
                 for (int k = 0; k < kLoads; k++)
                     if (k * kThreads < n_next * units)
-                        __builtin_memcpy(&read[k], frame + (uint64_t)(uint32_t)min(read_row[k], n_next - 1) * C.pitch + min(read_at[k], bytes - 16), 16);
+                        __builtin_memcpy(&read[k], frame + ((uint32_t)min(read_row[k], n_next - 1) * C.pitch + (uint32_t)min(read_at[k], bytes - 16)), 16);
             }
             if (f_next == 0) {
                 // Weights for 32 source rows a wave: lane l of a product holds rows 4 j + l / 16, j = 0 .. 7.
@@ -400,30 +409,41 @@ __global__ __launch_bounds__(kThreads, (Limits<kWide, (int)sizeof(T)>::workgroup
             const int run = part_rows * g.patch, tile_h = down * part_rows;  // of a patch's channel
             if (ok) {
                 if (lane < tile_w) {
-                    const int patch = (int)g.by_patch.quotient((uint32_t)lane), x_stage = patch * 3 * run + (lane - patch * g.patch);
-                    const int first = col_first[lane] - c0, taps = col_taps[lane], most = groups * 64 / 3;
-                    const float centre = col_centre[lane], norm = col_norm[lane];
+                    const int x_stage = patch * 3 * run + (x - patch * g.patch);
                     const int32_t *rows = row_stage + i * kTileRows;
-                    if (!kWide)
-                        sum_columns<T, kFewTaps, kSumPitch>(summed, stage, rows, tile_h, x_stage, first, taps, centre, inv_x, norm, most, run, g);
-                    else if (columns_of_window(C.scale_x, antialias) <= kSomeTaps)
-                        sum_columns<T, kSomeTaps, kSumPitch>(summed, stage, rows, tile_h, x_stage, first, taps, centre, inv_x, norm, most, run, g);
-                    else
-                        sum_columns<T, 0, kSumPitch>(summed, stage, rows, tile_h, x_stage, first, taps, centre, inv_x, norm, most, run, g);
+                    if (!any_taps) {
+                        sum_columns<T, kColumnTaps, kSumPitch, kWaves>(column, summed, stage, rows, tile_h, x_stage, run, g);
+                    } else {
+                        const Column<0> wide(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], 0);
+                        sum_columns<T, 0, kSumPitch, kWaves>(wide, summed, stage, rows, tile_h, x_stage, run, g);
+                    }
                 }
             } else {
                 for (int e = threadIdx.x; e < tile_w * tile_h * 3; e += kThreads) stage[e] = from_float<T>(0.0f);
             }
-            __syncthreads();
+        }
+        if (more && ok) {
+            // (the sums over rows are done with the samples before these)
+#pragma unroll
+            for (int k = 0; k < kLoads; k++) {
+                const int u = k * kThreads + (int)threadIdx.x;
+                if (!whole) read[k] = moved_back(read[k], max(read_at[k] - (bytes - 16), 0));
+                if (u < n_next * units) *reinterpret_cast<uint4 *>(raw + u * 16) = read[k];
+            }
+        }
+        __syncthreads();
+        if (f >= 0) {
+            // nothing waits for these: the next sums over columns follow a barrier, by which the values here are read
             for (int slot = f; slot < (f + 1 == distinct ? g.group : f + 1); slot++) {
                 T *o = out + slot * area + part_y0 * g.patch;
-                const int channel = g.group * area;
-                if (chunk == 16) write_runs<T, 16>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
-                else if (chunk == 8) write_runs<T, 8>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
-                else if (chunk == 4) write_runs<T, 4>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
-                else write_runs<T, (int)sizeof(T)>(stage, patch_row[i & 1], down * across * 3, run, o, out_stride, channel);
+                const int channel = g.group * area, runs = down * across * 3, stride = (int)out_stride;
+                const int32_t *rows = patch_row[i & 1];
+                const Divisor &chunks = part_rows == C.part_rows ? C.chunks : C.last_chunks;
+                if (chunk == 16) write_runs<T, 16, kThreads>(stage, rows, runs, chunks, o, stride, channel);
+                else if (chunk == 8) write_runs<T, 8, kThreads>(stage, rows, runs, chunks, o, stride, channel);
+                else if (chunk == 4) write_runs<T, 4, kThreads>(stage, rows, runs, chunks, o, stride, channel);
+                else write_runs<T, (int)sizeof(T), kThreads>(stage, rows, runs, chunks, o, stride, channel);
             }
-            __syncthreads();
         }
         if (!more) break;
         i = i_next;
@@ -538,25 +558,26 @@ bool patch_size(const prep_patch_params *p, int32_t width, int32_t height, int32
 
 // How a clip is cut into tiles, one way or the other; false = it is not.
 template <typename Most>
-bool cut_into_tiles(PatchClip *c, const PatchGeometry &g)
+bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
 {
-    if (c->width < kNarrowest) return false;
+    // (offsets inside a frame group are 32-bit)
+    if (c->width < kNarrowest || (int64_t)c->cols * c->rows * out_stride > INT32_MAX) return false;
     const double sx = g.antialias && c->scale_x > 1.0 ? c->scale_x : 1.0, sy = g.antialias && c->scale_y > 1.0 ? c->scale_y : 1.0;
     auto fits = [&](int across, int tall) {
         // at most so many source columns and rows lie under that many output samples in a row
         const int w = across * g.patch;
-        const double x = fmax((w - 1) * c->scale_x + 2.0 * sx + 2.0, (double)kNarrowest), y = (tall - 1) * c->scale_y + 2.0 * sy + 2.0;
+        const double x = 16.0 * ceil(((w - 1) * c->scale_x + 2.0 * sx + 1.0) / 16.0), y = (tall - 1) * c->scale_y + 2.0 * sy + 1.0;
         return w <= kTileCols && tall <= kTileRows && 3.0 * x <= (double)Most::span_bytes && y <= (double)Most::source_rows &&
-               y * (3.0 * x + 16.0) <= (double)Most::raw_bytes;
+               y * 3.0 * x <= (double)Most::raw_bytes;
     };
     c->parts = 1;
-    c->part_rows = g.patch;
+    c->part_rows = (uint16_t)g.patch;
     while (!fits(1, c->part_rows)) {
         if (c->part_rows <= 4) return false;
         c->parts++;
-        c->part_rows = (g.patch + c->parts - 1) / c->parts;
+        c->part_rows = (uint16_t)((g.patch + c->parts - 1) / c->parts);
     }
-    c->parts = (g.patch + c->part_rows - 1) / c->part_rows;
+    c->parts = (uint16_t)((g.patch + c->part_rows - 1) / c->part_rows);
     c->across = c->down = 1;
     while (c->across < c->cols && fits(c->across + 1, c->part_rows)) c->across++;
     if (c->parts == 1)
@@ -570,13 +591,13 @@ bool cut_into_tiles(PatchClip *c, const PatchGeometry &g)
 enum { kDirect = 0, kNarrow = 1, kWide = 2, kKinds = 3 };
 
 template <int kElement>
-int kind_of(PatchClip *c, const PatchGeometry &g)
+int kind_of(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
 {
     // The narrow kind keeps five workgroups on a compute unit where the wide one keeps three; what is reduced so far that its tiles
     // would be narrower than the other's is the wide kind's.
     PatchClip wide = *c;
-    const bool fits_wide = cut_into_tiles<Limits<true, kElement>>(&wide, g);
-    if (columns_of_window(c->scale_x, g.antialias) <= kFewTaps && cut_into_tiles<Limits<false, kElement>>(c, g) && (!fits_wide || c->across * c->down * c->part_rows >= wide.across * wide.down * wide.part_rows))
+    const bool fits_wide = cut_into_tiles<Limits<true, kElement>>(&wide, g, out_stride);
+    if (columns_of_window(c->scale_x, g.antialias) <= kFewTaps && cut_into_tiles<Limits<false, kElement>>(c, g, out_stride) && (!fits_wide || c->across * c->down * c->part_rows >= wide.across * wide.down * wide.part_rows))
         return kNarrow;
     *c = wide;
     return fits_wide ? kWide : kDirect;
@@ -589,15 +610,22 @@ uint64_t blocks_of(const PatchClip &c, const PatchGeometry &g, int kind)
     return ((uint64_t)c.cols * (uint64_t)c.rows * (uint64_t)(g.patch * g.patch) * groups_of(c, g) * (uint64_t)g.group + kThreads - 1) / kThreads;
 }
 
-// Bytes that all runs can be written by at a time.
-int chunk_bytes(const prep_patch_params *params, const ClipPack &pack, int n, const void *out, int64_t out_stride)
+// Bytes that all runs of the pack can be written by at a time, and the clips' divisors that go by it.
+int set_chunks(const prep_patch_params *params, ClipPack *pack, int n, const void *out, int64_t out_stride)
 {
     const uint64_t element = (uint64_t)element_bytes(params->out_dtype), p = (uint64_t)params->patch;
     uint64_t all = (uint64_t)(uintptr_t)out | (uint64_t)out_stride * element | p * p * element;
     for (int i = 0; i < n; i++)
-        if (pack.c[i].parts > 1) all |= (uint64_t)pack.c[i].part_rows * p * element;
+        if (pack->c[i].parts > 1) all |= (uint64_t)pack->c[i].part_rows * p * element;
     const uint64_t low = all & (~all + 1);
-    return (int)(low < 16 ? low : 16);
+    const int chunk = (int)(low < 16 ? low : 16);
+    for (int i = 0; i < n; i++) {
+        PatchClip &c = pack->c[i];
+        const int bytes = params->patch * (int)element, last = params->patch - (c.parts - 1) * c.part_rows;
+        c.chunks = divisor(c.part_rows * bytes / chunk);
+        c.last_chunks = divisor(last * bytes / chunk);
+    }
+    return chunk;
 }
 
 template <typename T>
@@ -605,9 +633,9 @@ void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, const
                 T *out, int64_t out_stride, hipStream_t stream)
 {
     if (kind == kWide)
-        hipLaunchKernelGGL((patch_rows_tiled<T, true>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
+        hipLaunchKernelGGL((patch_rows_tiled<T, true>), dim3(blocks), dim3(Limits<true, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
     else if (kind == kNarrow)
-        hipLaunchKernelGGL((patch_rows_tiled<T, false>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
+        hipLaunchKernelGGL((patch_rows_tiled<T, false>), dim3(blocks), dim3(Limits<false, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
     else
         hipLaunchKernelGGL((patch_rows_direct<T>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride);
 }
@@ -632,7 +660,7 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int3
     uint64_t tiles = 0;
     for (int32_t i = 0; i < n; i++) {
         PatchClip &c = clips[i];
-        kinds[i] = (uint8_t)(element_bytes(params->out_dtype) == 2 ? kind_of<2>(&c, g) : kind_of<4>(&c, g));
+        kinds[i] = (uint8_t)(element_bytes(params->out_dtype) == 2 ? kind_of<2>(&c, g, out_stride) : kind_of<4>(&c, g, out_stride));
         any[kinds[i]] = true;
         if (kinds[i] != kDirect) tiles += groups_of(c, g) * (uint64_t)c.tiles_x * (uint64_t)c.tiles_y;
     }
@@ -660,11 +688,11 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int3
                 m++;
             }
             if (m == 0) continue;
+            const int chunk = kind != kDirect ? set_chunks(params, &pack, m, out, out_stride) : 0;
             for (int k = m; k < kClips; k++) {
                 pack.c[k] = pack.c[0];
                 pack.block0[k] = 0xFFFFFFFFu;
             }
-            const int chunk = kind != kDirect ? chunk_bytes(params, pack, m, out, out_stride) : 0;
             if (params->out_dtype == PREP_F16)
                 launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (__half *)out, out_stride, stream);
             else if (params->out_dtype == PREP_BF16)
@@ -715,10 +743,10 @@ public:
         c.frame_stride = frame_stride;
         c.row0 = row_starts_[i];
         c.pitch = pitch;
-        c.width = width;
-        c.height = height;
-        c.cols = cols;
-        c.rows = rows;
+        c.width = (uint16_t)width;
+        c.height = (uint16_t)height;
+        c.cols = (uint16_t)cols;
+        c.rows = (uint16_t)rows;
         c.scale_x = (double)width / (double)(cols * params_->patch);
         c.scale_y = (double)height / (double)(rows * params_->patch);
         c.frames = frames;
