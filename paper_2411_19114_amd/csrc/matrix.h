@@ -1,21 +1,18 @@
 // The matrix instruction that the patch rows use, and its operands (gfx950).
 #ifndef PREP_MATRIX_H
 #define PREP_MATRIX_H
-#include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 namespace prep {
 
-// The values of byte i of r0 and of r1, times 2^-9, as two halves.  A half whose low byte is b and whose high byte is 0 is the
-// subnormal b 2^-24; the product with 2^15 is exact.
+// The values of byte i of r0 and of r1, times 2^-24, as two halves: a half whose low byte is b and whose high byte is 0 is the
+// subnormal b 2^-24, which the product below takes as it is.
 __device__ __forceinline__ uint32_t byte_pair(uint32_t r0, uint32_t r1, int i)
 {
-    const uint32_t both = __builtin_amdgcn_perm(r1, r0, 0x0C040C00u + (uint32_t)i * 0x00010001u);
-    const __half2 scaled = __hmul2(__builtin_bit_cast(__half2, both), __floats2half2_rn(32768.0f, 32768.0f));
-    return __builtin_bit_cast(uint32_t, scaled);
+    return __builtin_amdgcn_perm(r1, r0, 0x0C040C00u + (uint32_t)i * 0x00010001u);
 }
-constexpr float kBytePairScale = 1.0f / 512.0f;
+constexpr float kBytePairScale = 1.0f / 16777216.0f;
 
 // c + a b, fp32 sums of products of halves.  a: 16 rows of 32, lane l holds eight values of row l mod 16; b: 32 of 16 columns, lane l
 // holds eight values of column l mod 16; which eight of the 32 a lane holds depends on l / 16 alone, in the same way for both.  c and

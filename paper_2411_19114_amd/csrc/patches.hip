@@ -332,16 +332,23 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
                     for (int j = 0; j < 4; j++) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
                     for (int step = 0; step < Most::steps && 32 * step < n_rows; step++) {
-                        uint32_t b[8];
+                        // (pairs of rows behind the last one are left out; a row behind it in a pair has weight 0)
+                        uint32_t pair[4][4];
 #pragma unroll
-                        for (int j = 0; j < 8; j++) {
-                            const int k = min(32 * step + 4 * j + (lane >> 4), n_rows - 1);  // (weight 0 behind the last row)
-                            b[j] = *reinterpret_cast<const uint32_t *>(raw + k * raw_pitch + at);
+                        for (int p = 0; p < 4; p++) {
+                            pair[0][p] = pair[1][p] = pair[2][p] = pair[3][p] = 0;
+                            if (32 * step + 8 * p < n_rows) {
+                                const int k = 32 * step + 8 * p + (lane >> 4);
+                                const uint32_t r0 = *reinterpret_cast<const uint32_t *>(raw + min(k, n_rows - 1) * raw_pitch + at);
+                                const uint32_t r1 = *reinterpret_cast<const uint32_t *>(raw + min(k + 4, n_rows - 1) * raw_pitch + at);
+#pragma unroll
+                                for (int j = 0; j < 4; j++) pair[j][p] = byte_pair(r0, r1, j);
+                            }
                         }
                         const uint4 hi = weight[step][0][lane], lo = weight[step][1][lane];
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
-                            const uint4 column = make_uint4(byte_pair(b[0], b[1], j), byte_pair(b[2], b[3], j), byte_pair(b[4], b[5], j), byte_pair(b[6], b[7], j));
+                            const uint4 column = make_uint4(pair[j][0], pair[j][1], pair[j][2], pair[j][3]);
                             sum[j] = multiply_add_16x16x32(lo, column, multiply_add_16x16x32(hi, column, sum[j]));
                         }
                     }
@@ -376,12 +383,13 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
                         __builtin_memcpy(&read[k], frame + ((uint32_t)min(read_row[k], n_next - 1) * C.pitch + (uint32_t)min(read_at[k], bytes - 16)), 16);
             }
             if (f_next == 0) {
-                // Weights for 32 source rows a wave: lane l of a product holds rows 4 j + l / 16, j = 0 .. 7.
-                const int m = lane & 15;
-                if (32 * wave < n_next) {
+                // Weights for 32 source rows a wave, the last ones (which have fewer rows to finish where these do not divide
+                // evenly): lane l of a product holds rows 4 j + l / 16, j = 0 .. 7.
+                const int m = lane & 15, step = kWaves - 1 - wave;
+                if (32 * step < n_next) {
                     uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
                     if (m < down_next * part_rows_next) {
-                        const int begin = row_first[row + m] - r0 - 32 * wave - (lane >> 4), n = row_taps[row + m];
+                        const int begin = row_first[row + m] - r0 - 32 * step - (lane >> 4), n = row_taps[row + m];
                         const float centre = row_centre[row + m], scale = row_norm[row + m];
 #pragma unroll
                         for (int j = 0; j < 8; j++) {
@@ -396,8 +404,8 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
                             lo[j >> 1] |= (uint32_t)rb << (16 * (j & 1));
                         }
                     }
-                    weight[wave][0][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    weight[wave][1][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    weight[step][0][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    weight[step][1][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 }
                 for (int p = threadIdx.x; p < down_next * across; p += kThreads) {
                     const int a = down_next == 1 ? 0 : p / across;

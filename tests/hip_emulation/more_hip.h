@@ -41,12 +41,8 @@ inline void __builtin_amdgcn_wave_barrier()
 // csrc/matrix.h on the CPU: the same operands, products and sums in the order of the 32
 #define PREP_MATRIX_H
 namespace prep {
-inline uint32_t byte_pair(uint32_t r0, uint32_t r1, int i)
-{
-    const float a = (float)(r0 >> (8 * i) & 255u) / 512.0f, b = (float)(r1 >> (8 * i) & 255u) / 512.0f;
-    return (uint32_t)__float2half_rn(a).x | (uint32_t)__float2half_rn(b).x << 16;
-}
-constexpr float kBytePairScale = 1.0f / 512.0f;
+inline uint32_t byte_pair(uint32_t r0, uint32_t r1, int i) { return (r0 >> (8 * i) & 255u) | (r1 >> (8 * i) & 255u) << 16; }
+constexpr float kBytePairScale = 1.0f / 16777216.0f;
 
 inline float4 multiply_add_16x16x32(uint4 a, uint4 b, float4 c)
 {
