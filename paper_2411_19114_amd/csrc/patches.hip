@@ -26,7 +26,7 @@ namespace prep {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kClips = 32;  // clips of one launch: their records are kernel arguments (3 KB), so that a call has
+constexpr int kClips = 64;  // clips of one launch: their records are kernel arguments (4 KB), so that a call has
                             // no workspace, calls may overlap and a captured call keeps its own
 
 // Division by a number that the host knows: the quotient by a multiplication is right or one too large.
@@ -38,7 +38,8 @@ struct Divisor {
         return d == 1 ? n : q - (q * d > n ? 1u : 0u);
     }
 };
-inline Divisor divisor(int d) { return {(uint32_t)d, (uint32_t)((0x100000000ull + (uint64_t)d - 1) / (uint64_t)d)}; }
+// (2^32 - 1) / d + 1 = 2^32 / d rounded up, modulo 2^32
+__host__ __device__ __forceinline__ Divisor divisor(int d) { return {(uint32_t)d, 0xFFFFFFFFu / (uint32_t)d + 1u}; }
 
 // A tile's limits, for clips whose windows hold at most kFewTaps columns (kWide = false) and for the others.
 constexpr int kTileCols = 64, kTileRows = 16, kPatches = 128;
@@ -61,29 +62,33 @@ struct PatchClip {
     uint64_t src_off;       // first byte of its first frame
     uint64_t frame_stride;  // bytes
     int64_t row0;           // its first row
-    double scale_x, scale_y;  // source samples per output sample
     uint32_t pitch;
-    uint16_t width, height; // pixels
-    uint16_t cols, rows;    // patches
     int32_t frames;
     int32_t image;          // index into `status`
+    uint32_t strips_m;      // Divisors' m: strips of a frame group, and of a row of them
+    uint32_t strips_x_m;
+    uint16_t width, height; // pixels
+    uint16_t cols, rows;    // patches
     // tiles: patches across and down, rows of a patch in it (fewer than the patch has where that is tall: `parts` tiles
-    // share a patch then), tiles across and down; strips of tiles across and down
-    uint16_t across, down, part_rows, parts;
-    int32_t tiles_x, tiles_y;
-    Divisor strips_x, strips;  // in a row of them; of a frame group
-    Divisor chunks, last_chunks;  // written at a time, of a patch's channel in a tile; in the last tile of a patch
+    // share a patch then)
+    uint8_t across, down, part_rows, parts;
+    __host__ __device__ int tiles_x() const { return (cols + across - 1) / across; }
+    __host__ __device__ int tiles_y() const { return (rows + down - 1) / down * parts; }
+    // source samples per output sample
+    __host__ __device__ double scale_x(int patch) const { return (double)width / (double)(cols * patch); }
+    __host__ __device__ double scale_y(int patch) const { return (double)height / (double)(rows * patch); }
 };
 struct ClipPack {
     uint32_t block0[kClips];  // first workgroup of each clip; of those that the launch lacks 2^32 - 1
     PatchClip c[kClips];
 };
-static_assert(sizeof(ClipPack) <= 3968, "kernel arguments are 4 KB at most");
+static_assert(sizeof(ClipPack) <= 3976, "kernel arguments are 4 KB at most");
 struct PatchGeometry {
     int32_t patch, merge, group;  // pixels, patches, frames
     int32_t antialias;
     int32_t strip;                // tiles of a workgroup
-    Divisor by_patch, by_merge;
+    int32_t chunk;                // bytes written at a time
+    Divisor by_patch, by_merge, by_chunks;  // (chunks of a patch's channel)
     float scale[3], bias[3];      // 1 / (255 std), -mean / std
 };
 
@@ -94,7 +99,7 @@ struct Taps {
     float inv;     // 1 / s
     __device__ __forceinline__ float weight(int k) const { return fmaxf(0.0f, fmaf(-fabsf((float)k - centre), inv, 1.0f)); }
 };
-__host__ __device__ __forceinline__ Taps make_taps(int i, int size, double scale, bool antialias)
+__host__ __device__ __forceinline__ Taps make_taps(int i, int size, double scale, float inv, bool antialias)
 {
     // in 64 bits: a coordinate near 2000 would leave a float 13 bits of fraction
     const double c = ((double)i + 0.5) * scale - 0.5, s = antialias && scale > 1.0 ? scale : 1.0;
@@ -102,17 +107,20 @@ __host__ __device__ __forceinline__ Taps make_taps(int i, int size, double scale
     t.first = max((int)floor(c - s) + 1, 0);  // (weight 0 at c - s itself)
     t.end = min((int)ceil(c + s), size);
     t.centre = (float)(c - (double)t.first);
-    t.inv = (float)(1.0 / s);
+    t.inv = inv;
     return t;
 }
 
-// (without a branch: scalar loads of the whole list go out together)
+// (eight entries at a time without a branch: their scalar loads go out together)
 __device__ __forceinline__ int clip_of(const ClipPack &pack, uint32_t block)
 {
-    int i = 0;
+    static_assert(kClips == 64, "two steps of eight");
+    int i = 0, k = 0;
 #pragma unroll
-    for (int k = 1; k < kClips; k++) i += pack.block0[k] <= block ? 1 : 0;
-    return i;
+    for (int e = 1; e < 8; e++) i += pack.block0[8 * e] <= block ? 8 : 0;
+#pragma unroll
+    for (int e = 1; e < 8; e++) k += pack.block0[i + e] <= block ? 1 : 0;
+    return i + k;
 }
 
 // Row, inside its group of frames, of patch (py, px): row_of_line(py) + row_of_column(px).
@@ -222,8 +230,7 @@ __device__ __forceinline__ void sum_columns(const Column<kTaps> &column, const f
 
 template <typename T, bool kWide>
 __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<kWide, (int)sizeof(T)>::waves / 4 * Limits<kWide, (int)sizeof(T)>::workgroups)) void patch_rows_tiled(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
-                                                             const int32_t *__restrict__ status, T *__restrict__ out, int64_t out_stride,
-                                                             int chunk)
+                                                             const int32_t *__restrict__ status, T *__restrict__ out, int64_t out_stride)
 {
     typedef Limits<kWide, (int)sizeof(T)> Most;
     constexpr int kSumPitch = Most::sum_pitch, kLoads = Most::loads, kThreads = Most::threads, kWaves = Most::waves;
@@ -240,19 +247,22 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
     const int clip = clip_of(pack, blockIdx.x);
     const PatchClip &C = pack.c[clip];
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    const uint32_t strip = blockIdx.x - pack.block0[clip], frames_group = C.strips.quotient(strip);
-    const uint32_t in_group = strip - frames_group * C.strips.d, strip_y = C.strips_x.quotient(in_group);
-    const int tile_x = (int)(in_group - strip_y * C.strips_x.d), tile_y0 = (int)strip_y * g.strip;
-    const int tiles = min(g.strip, C.tiles_y - tile_y0);
+    const int tiles_x = C.tiles_x(), tiles_y = C.tiles_y();
+    const Divisor strips = {(uint32_t)(tiles_x * ((tiles_y + g.strip - 1) / g.strip)), C.strips_m}, strips_x = {(uint32_t)tiles_x, C.strips_x_m};
+    const uint32_t strip = blockIdx.x - pack.block0[clip], frames_group = strips.quotient(strip);
+    const uint32_t in_group = strip - frames_group * strips.d, strip_y = strips_x.quotient(in_group);
+    const int tile_x = (int)(in_group - strip_y * strips_x.d), tile_y0 = (int)strip_y * g.strip;
+    const int tiles = min(g.strip, tiles_y - tile_y0);
     const int px0 = tile_x * C.across, across = min((int)C.across, C.cols - px0);  // patches
     const int tile_w = across * g.patch, x0 = px0 * g.patch;
     const bool antialias = g.antialias != 0;
-    const float inv_x = (float)(1.0 / (antialias && C.scale_x > 1.0 ? C.scale_x : 1.0));
-    const float inv_y = (float)(1.0 / (antialias && C.scale_y > 1.0 ? C.scale_y : 1.0));
+    // 1 / s
+    const float inv_x = antialias ? fminf((float)(C.cols * g.patch) / (float)C.width, 1.0f) : 1.0f;
+    const float inv_y = antialias ? fminf((float)(C.rows * g.patch) / (float)C.height, 1.0f) : 1.0f;
 
     if (wave == 0) {
         if (lane < tile_w) {
-            const Taps w = make_taps(x0 + lane, C.width, C.scale_x, antialias);
+            const Taps w = make_taps(x0 + lane, C.width, C.scale_x(g.patch), inv_x, antialias);
             float sum = 0.0f;
             for (int k = 0; k < w.end - w.first; k++) sum += w.weight(k);
             col_first[lane] = w.first;
@@ -272,7 +282,7 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
         if (i < tiles) {
             if (t < down) line_row[lane] = row_of_line(g, py0 + t, C.cols);
             if (t < down * part_rows) {
-                const Taps w = make_taps(py0 * g.patch + part_y0 + t, C.height, C.scale_y, antialias);
+                const Taps w = make_taps(py0 * g.patch + part_y0 + t, C.height, C.scale_y(g.patch), inv_y, antialias);
                 float sum = 0.0f;
                 for (int k = 0; k < w.end - w.first; k++) sum += w.weight(k);
                 row_first[lane] = w.first;
@@ -316,8 +326,15 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
     // the lane's output column
     constexpr int kColumnTaps = kWide ? kSomeTaps : kFewTaps;
     const int x = min(lane, tile_w - 1), patch = (int)g.by_patch.quotient((uint32_t)x);
-    const bool any_taps = kWide && columns_of_window(C.scale_x, antialias) > kSomeTaps;
+    const bool any_taps = kWide && antialias && 2 * (int)C.width >= kSomeTaps * C.cols * g.patch;  // (columns_of_window > kSomeTaps)
     const Column<kColumnTaps> column(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], groups * 64 / 3);
+
+    // what is written at a time, of a patch's channel in a tile, and in the last tile of a patch that several share
+    Divisor whole_part = g.by_chunks, last_part = g.by_chunks;
+    if (C.parts > 1) {
+        whole_part = divisor(C.part_rows * g.patch * (int)sizeof(T) / g.chunk);
+        last_part = divisor((g.patch - (C.parts - 1) * C.part_rows) * g.patch * (int)sizeof(T) / g.chunk);
+    }
 
     // Tile i, frame f is worked on while the frame after it is read; before the first, nothing is.
     int i = 0, f = -1, n_rows = 0, down = 0, part_rows = 0, part_y0 = 0;
@@ -446,10 +463,10 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
                 T *o = out + slot * area + part_y0 * g.patch;
                 const int channel = g.group * area, runs = down * across * 3, stride = (int)out_stride;
                 const int32_t *rows = patch_row[i & 1];
-                const Divisor &chunks = part_rows == C.part_rows ? C.chunks : C.last_chunks;
-                if (chunk == 16) write_runs<T, 16, kThreads>(stage, rows, runs, chunks, o, stride, channel);
-                else if (chunk == 8) write_runs<T, 8, kThreads>(stage, rows, runs, chunks, o, stride, channel);
-                else if (chunk == 4) write_runs<T, 4, kThreads>(stage, rows, runs, chunks, o, stride, channel);
+                const Divisor &chunks = part_rows == C.part_rows ? whole_part : last_part;
+                if (g.chunk == 16) write_runs<T, 16, kThreads>(stage, rows, runs, chunks, o, stride, channel);
+                else if (g.chunk == 8) write_runs<T, 8, kThreads>(stage, rows, runs, chunks, o, stride, channel);
+                else if (g.chunk == 4) write_runs<T, 4, kThreads>(stage, rows, runs, chunks, o, stride, channel);
                 else write_runs<T, (int)sizeof(T), kThreads>(stage, rows, runs, chunks, o, stride, channel);
             }
         }
@@ -486,7 +503,9 @@ __global__ __launch_bounds__(kThreads) void patch_rows_direct(const uint8_t *__r
     const int y = py * g.patch + in_patch / g.patch, x = px * g.patch + in_patch % g.patch;
     float v[3] = {0.0f, 0.0f, 0.0f};
     if (status == nullptr || status[C.image] == PREP_OK) {
-        const Taps ty = make_taps(y, C.height, C.scale_y, g.antialias), tx = make_taps(x, C.width, C.scale_x, g.antialias);
+        const float inv_y = g.antialias ? fminf((float)(rows * g.patch) / (float)C.height, 1.0f) : 1.0f;
+        const float inv_x = g.antialias ? fminf((float)(cols * g.patch) / (float)C.width, 1.0f) : 1.0f;
+        const Taps ty = make_taps(y, C.height, C.scale_y(g.patch), inv_y, g.antialias), tx = make_taps(x, C.width, C.scale_x(g.patch), inv_x, g.antialias);
         const uint8_t *src = rgb + C.src_off + (uint64_t)f * C.frame_stride;
         float sum_x = 0.0f, sum_y = 0.0f;
         for (int k = 0; k < tx.end - tx.first; k++) sum_x += tx.weight(k);
@@ -570,80 +589,78 @@ bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
 {
     // (offsets inside a frame group are 32-bit)
     if (c->width < kNarrowest || (int64_t)c->cols * c->rows * out_stride > INT32_MAX) return false;
-    const double sx = g.antialias && c->scale_x > 1.0 ? c->scale_x : 1.0, sy = g.antialias && c->scale_y > 1.0 ? c->scale_y : 1.0;
+    const double scale_x = c->scale_x(g.patch), scale_y = c->scale_y(g.patch);
+    const double sx = g.antialias && scale_x > 1.0 ? scale_x : 1.0, sy = g.antialias && scale_y > 1.0 ? scale_y : 1.0;
     auto fits = [&](int across, int tall) {
         // at most so many source columns and rows lie under that many output samples in a row
         const int w = across * g.patch;
-        const double x = 16.0 * ceil(((w - 1) * c->scale_x + 2.0 * sx + 1.0) / 16.0), y = (tall - 1) * c->scale_y + 2.0 * sy + 1.0;
+        const double x = 16.0 * ceil(((w - 1) * scale_x + 2.0 * sx + 1.0) / 16.0), y = (tall - 1) * scale_y + 2.0 * sy + 1.0;
         return w <= kTileCols && tall <= kTileRows && 3.0 * x <= (double)Most::span_bytes && y <= (double)Most::source_rows &&
                y * 3.0 * x <= (double)Most::raw_bytes;
     };
     c->parts = 1;
-    c->part_rows = (uint16_t)g.patch;
+    c->part_rows = (uint8_t)g.patch;
     while (!fits(1, c->part_rows)) {
         if (c->part_rows <= 4) return false;
         c->parts++;
-        c->part_rows = (uint16_t)((g.patch + c->parts - 1) / c->parts);
+        c->part_rows = (uint8_t)((g.patch + c->parts - 1) / c->parts);
     }
-    c->parts = (uint16_t)((g.patch + c->part_rows - 1) / c->part_rows);
+    c->parts = (uint8_t)((g.patch + c->part_rows - 1) / c->part_rows);
     c->across = c->down = 1;
     while (c->across < c->cols && fits(c->across + 1, c->part_rows)) c->across++;
     if (c->parts == 1)
         while (c->down < c->rows && (c->down + 1) * c->across <= kPatches && fits(c->across, (c->down + 1) * g.patch)) c->down++;
-    c->tiles_x = (c->cols + c->across - 1) / c->across;
-    c->tiles_y = (c->rows + c->down - 1) / c->down * c->parts;
     return true;
 }
 
 // The kernels: patch_rows_direct, patch_rows_tiled with kWide = false and true.
 enum { kDirect = 0, kNarrow = 1, kWide = 2, kKinds = 3 };
 
+// Cuts the clips of a call into tiles.  One launch takes them all (two would wait for each other's last workgroups, 10 us or more), of the narrow kind where
+// every clip's tiles are as large as the wide kind's: it keeps four workgroups on a compute unit where the wide one keeps two.
 template <int kElement>
-int kind_of(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
+void cut_clips(PatchClip *clips, uint8_t *kinds, int32_t n, const PatchGeometry &g, int64_t out_stride)
 {
-    // The narrow kind keeps five workgroups on a compute unit where the wide one keeps three; what is reduced so far that its tiles
-    // would be narrower than the other's is the wide kind's.
-    PatchClip wide = *c;
-    const bool fits_wide = cut_into_tiles<Limits<true, kElement>>(&wide, g, out_stride);
-    if (columns_of_window(c->scale_x, g.antialias) <= kFewTaps && cut_into_tiles<Limits<false, kElement>>(c, g, out_stride) && (!fits_wide || c->across * c->down * c->part_rows >= wide.across * wide.down * wide.part_rows))
-        return kNarrow;
-    *c = wide;
-    return fits_wide ? kWide : kDirect;
+    bool narrow = true;
+    for (int32_t i = 0; i < n; i++) {
+        PatchClip &c = clips[i], other = c;
+        kinds[i] = cut_into_tiles<Limits<true, kElement>>(&c, g, out_stride) ? kWide : kDirect;
+        if (kinds[i] == kWide)
+            narrow = narrow && columns_of_window(c.scale_x(g.patch), g.antialias) <= kFewTaps && cut_into_tiles<Limits<false, kElement>>(&other, g, out_stride) &&
+                     other.across * other.down * other.part_rows >= c.across * c.down * c.part_rows;
+    }
+    if (!narrow) return;
+    for (int32_t i = 0; i < n; i++)
+        if (kinds[i] == kWide && cut_into_tiles<Limits<false, kElement>>(&clips[i], g, out_stride)) kinds[i] = kNarrow;
 }
 
 uint64_t groups_of(const PatchClip &c, const PatchGeometry &g) { return (uint64_t)((c.frames - 1) / g.group + 1); }
+int strips_of(const PatchClip &c, const PatchGeometry &g) { return c.tiles_x() * ((c.tiles_y() + g.strip - 1) / g.strip); }
 uint64_t blocks_of(const PatchClip &c, const PatchGeometry &g, int kind)
 {
-    if (kind != kDirect) return groups_of(c, g) * c.strips.d;
+    if (kind != kDirect) return groups_of(c, g) * (uint64_t)strips_of(c, g);
     return ((uint64_t)c.cols * (uint64_t)c.rows * (uint64_t)(g.patch * g.patch) * groups_of(c, g) * (uint64_t)g.group + kThreads - 1) / kThreads;
 }
 
-// Bytes that all runs of the pack can be written by at a time, and the clips' divisors that go by it.
-int set_chunks(const prep_patch_params *params, ClipPack *pack, int n, const void *out, int64_t out_stride)
+// Bytes that all runs can be written by at a time.
+int chunk_bytes(const prep_patch_params *params, const PatchClip *clips, int32_t n, const void *out, int64_t out_stride)
 {
     const uint64_t element = (uint64_t)element_bytes(params->out_dtype), p = (uint64_t)params->patch;
     uint64_t all = (uint64_t)(uintptr_t)out | (uint64_t)out_stride * element | p * p * element;
-    for (int i = 0; i < n; i++)
-        if (pack->c[i].parts > 1) all |= (uint64_t)pack->c[i].part_rows * p * element;
+    for (int32_t i = 0; i < n; i++)
+        if (clips[i].parts > 1) all |= (uint64_t)clips[i].part_rows * p * element;
     const uint64_t low = all & (~all + 1);
-    const int chunk = (int)(low < 16 ? low : 16);
-    for (int i = 0; i < n; i++) {
-        PatchClip &c = pack->c[i];
-        const int bytes = params->patch * (int)element, last = params->patch - (c.parts - 1) * c.part_rows;
-        c.chunks = divisor(c.part_rows * bytes / chunk);
-        c.last_chunks = divisor(last * bytes / chunk);
-    }
-    return chunk;
+    return (int)(low < 16 ? low : 16);
 }
 
 template <typename T>
-void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, const PatchGeometry &g, int kind, int chunk, const int32_t *status,
+void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, const PatchGeometry &g, int kind, const int32_t *status,
                 T *out, int64_t out_stride, hipStream_t stream)
 {
     if (kind == kWide)
-        hipLaunchKernelGGL((patch_rows_tiled<T, true>), dim3(blocks), dim3(Limits<true, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
+        hipLaunchKernelGGL((patch_rows_tiled<T, true>), dim3(blocks), dim3(Limits<true, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride);
     else if (kind == kNarrow)
-        hipLaunchKernelGGL((patch_rows_tiled<T, false>), dim3(blocks), dim3(Limits<false, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride, chunk);
+        hipLaunchKernelGGL((patch_rows_tiled<T, false>), dim3(blocks), dim3(Limits<false, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride);
     else
         hipLaunchKernelGGL((patch_rows_direct<T>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride);
 }
@@ -664,21 +681,24 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int3
         g.scale[c] = (float)(1.0 / (255.0 * (double)params->std[c]));
         g.bias[c] = (float)(-(double)params->mean[c] / (double)params->std[c]);
     }
+    if (element_bytes(params->out_dtype) == 2) cut_clips<2>(clips, kinds, n, g, out_stride);
+    else cut_clips<4>(clips, kinds, n, g, out_stride);
+    g.chunk = chunk_bytes(params, clips, n, out, out_stride);
+    g.by_chunks = divisor(g.patch * g.patch * element_bytes(params->out_dtype) / g.chunk);
     bool any[kKinds] = {false, false, false};
     uint64_t tiles = 0;
     for (int32_t i = 0; i < n; i++) {
         PatchClip &c = clips[i];
-        kinds[i] = (uint8_t)(element_bytes(params->out_dtype) == 2 ? kind_of<2>(&c, g, out_stride) : kind_of<4>(&c, g, out_stride));
         any[kinds[i]] = true;
-        if (kinds[i] != kDirect) tiles += groups_of(c, g) * (uint64_t)c.tiles_x * (uint64_t)c.tiles_y;
+        if (kinds[i] != kDirect) tiles += groups_of(c, g) * (uint64_t)c.tiles_x() * (uint64_t)c.tiles_y();
     }
     // a workgroup takes a strip of tiles where there are plenty, so that it can read one while it works on another
     g.strip = (int)(tiles / 1536 < 1 ? 1 : tiles / 1536 > kStrip ? kStrip : tiles / 1536);
     for (int32_t i = 0; i < n; i++) {
         PatchClip &c = clips[i];
         if (kinds[i] == kDirect) continue;
-        c.strips_x = divisor(c.tiles_x);
-        c.strips = divisor(c.tiles_x * ((c.tiles_y + g.strip - 1) / g.strip));
+        c.strips_x_m = divisor(c.tiles_x()).m;
+        c.strips_m = divisor(strips_of(c, g)).m;
     }
     for (int kind = 0; kind < kKinds; kind++) {
         if (!any[kind]) continue;
@@ -696,17 +716,16 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int3
                 m++;
             }
             if (m == 0) continue;
-            const int chunk = kind != kDirect ? set_chunks(params, &pack, m, out, out_stride) : 0;
             for (int k = m; k < kClips; k++) {
                 pack.c[k] = pack.c[0];
                 pack.block0[k] = 0xFFFFFFFFu;
             }
             if (params->out_dtype == PREP_F16)
-                launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (__half *)out, out_stride, stream);
+                launch_for(rgb, pack, (uint32_t)blocks, g, kind, status, (__half *)out, out_stride, stream);
             else if (params->out_dtype == PREP_BF16)
-                launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (__hip_bfloat16 *)out, out_stride, stream);
+                launch_for(rgb, pack, (uint32_t)blocks, g, kind, status, (__hip_bfloat16 *)out, out_stride, stream);
             else
-                launch_for(rgb, pack, (uint32_t)blocks, g, kind, chunk, status, (float *)out, out_stride, stream);
+                launch_for(rgb, pack, (uint32_t)blocks, g, kind, status, (float *)out, out_stride, stream);
         }
     }
     return PREP_OK;
@@ -755,8 +774,7 @@ public:
         c.height = (uint16_t)height;
         c.cols = (uint16_t)cols;
         c.rows = (uint16_t)rows;
-        c.scale_x = (double)width / (double)(cols * params_->patch);
-        c.scale_y = (double)height / (double)(rows * params_->patch);
+        c.across = c.down = c.part_rows = c.parts = 1;  // (direct)
         c.frames = frames;
         c.image = i;
         row_starts_[i + 1] = row_starts_[i] + groups * rows * cols;
