@@ -45,7 +45,7 @@ __host__ __device__ __forceinline__ Divisor divisor(int d) { return {(uint32_t)d
 constexpr int kTileCols = 64, kTileRows = 16, kPatches = 128;
 constexpr int kStrip = 4;                          // tiles one below the other that a workgroup takes, at most
 constexpr int kNarrowest = 6;                      // narrowest image whose rows hold a read of 16 bytes
-constexpr int kFewTaps = 3, kSomeTaps = 6;          // columns of a window whose weights stay in registers
+constexpr int kFewTaps = 3, kSomeTaps = 5;          // columns of a window whose weights stay in registers
 constexpr float kWeightScale = 32768.0f;
 template <bool kWide, int kElement>
 struct Limits {
@@ -591,25 +591,40 @@ bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
     if (c->width < kNarrowest || (int64_t)c->cols * c->rows * out_stride > INT32_MAX) return false;
     const double scale_x = c->scale_x(g.patch), scale_y = c->scale_y(g.patch);
     const double sx = g.antialias && scale_x > 1.0 ? scale_x : 1.0, sy = g.antialias && scale_y > 1.0 ? scale_y : 1.0;
-    auto fits = [&](int across, int tall) {
-        // at most so many source columns and rows lie under that many output samples in a row
-        const int w = across * g.patch;
-        const double x = 16.0 * ceil(((w - 1) * scale_x + 2.0 * sx + 1.0) / 16.0), y = (tall - 1) * scale_y + 2.0 * sy + 1.0;
-        return w <= kTileCols && tall <= kTileRows && 3.0 * x <= (double)Most::span_bytes && y <= (double)Most::source_rows &&
-               y * 3.0 * x <= (double)Most::raw_bytes;
+    // Under n output samples in a row lie fewer than (n - 1) scale + 2 s + 1 source samples; columns come in sixteens.
+    const auto rows_under = [&](int n) { return (n - 1) * scale_y + 2.0 * sy + 1.0; };
+    // the most output samples over at most `most` source samples
+    const auto over = [](double most, double scale, double s) {
+        const double n = floor((most - 2.0 * s - 1.0) / scale) + 1.0;
+        return n < 0.0 ? 0 : n > 65535.0 ? 65535 : (int)n;
+    };
+    const auto columns_over = [&](int tall) {  // pixels across where the tile is `tall` pixels high; 0 = too many rows lie under it
+        const double y = rows_under(tall);
+        if (tall > kTileRows || y > (double)Most::source_rows) return 0;
+        const double most = fmin(Most::span_bytes / 48 * 16.0, 16.0 * floor(Most::raw_bytes / (48.0 * y)));
+        const int w = over(most, scale_x, sx);
+        return w < kTileCols ? w : kTileCols;
     };
     c->parts = 1;
     c->part_rows = (uint8_t)g.patch;
-    while (!fits(1, c->part_rows)) {
+    int across;
+    while ((across = columns_over(c->part_rows) / g.patch) < 1) {
         if (c->part_rows <= 4) return false;
         c->parts++;
         c->part_rows = (uint8_t)((g.patch + c->parts - 1) / c->parts);
     }
     c->parts = (uint8_t)((g.patch + c->part_rows - 1) / c->part_rows);
-    c->across = c->down = 1;
-    while (c->across < c->cols && fits(c->across + 1, c->part_rows)) c->across++;
-    if (c->parts == 1)
-        while (c->down < c->rows && (c->down + 1) * c->across <= kPatches && fits(c->across, (c->down + 1) * g.patch)) c->down++;
+    c->across = (uint8_t)(across < c->cols ? across : c->cols);
+    if (c->across > kPatches) c->across = kPatches;
+    c->down = 1;
+    if (c->parts == 1) {
+        const double x = 16.0 * ceil(((c->across * g.patch - 1) * scale_x + 2.0 * sx + 1.0) / 16.0);
+        const int tall = over(fmin((double)Most::source_rows, Most::raw_bytes / (3.0 * x)), scale_y, sy);
+        int down = (tall < kTileRows ? tall : kTileRows) / g.patch;
+        if (down > kPatches / c->across) down = kPatches / c->across;
+        if (down > c->rows) down = c->rows;
+        if (down > 1) c->down = (uint8_t)down;
+    }
     return true;
 }
 
