@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void rotary_pairs(prep_rotary_args A, Rot
 }
 
 // Aligned rows.  A lane takes 32 bytes of a head's row in two loads of 16 (kHalves: values i.. and i + n.., whose pairs meet in
-// the lane), always the same places of a row, and kRows rows one after the other whose loads go out together, before the
+// the lane), always the same places of a row, and kRows rows whose loads go out together, before the
 // angles are formed.  A token's angles are formed once per workgroup and shared by all its heads.
 struct RowShape {
     int32_t units;           // lanes of a row
@@ -136,7 +136,25 @@ union Vec {
     T v[16 / sizeof(T)];
 };
 
-template <typename T, bool kHalves, int kRows>
+// 16 bytes; kStream: which nobody reads again before the caches have seen as much as they hold.
+template <bool kStream>
+__device__ __forceinline__ uint4 load16(const void *p)
+{
+    typedef uint32_t Four __attribute__((vector_size(16)));
+    if (!kStream) return *static_cast<const uint4 *>(p);
+    const Four v = __builtin_nontemporal_load(static_cast<const Four *>(p));
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+template <bool kStream>
+__device__ __forceinline__ void store16(void *p, uint4 v)
+{
+    typedef uint32_t Four __attribute__((vector_size(16)));
+    const Four f = {v.x, v.y, v.z, v.w};
+    if (kStream) __builtin_nontemporal_store(f, static_cast<Four *>(p));
+    else *static_cast<uint4 *>(p) = v;
+}
+
+template <typename T, bool kHalves, int kRows, bool kStream>
 __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowShape S, const uint64_t *__restrict__ turns)
 {
     constexpr int kV = 16 / (int)sizeof(T);
@@ -181,8 +199,8 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowS
                 const int64_t ts = of_k < 0 ? A.q.token_stride : of_v < 0 ? A.k.token_stride : A.v.token_stride;
                 const int64_t hs = of_k < 0 ? A.q.head_stride : of_v < 0 ? A.k.head_stride : A.v.head_stride;
                 const T *src = base + (token0 + t) * ts + (of_k < 0 ? h : of_v < 0 ? of_k : of_v) * hs;
-                a[k].raw = *reinterpret_cast<const uint4 *>(src + at_a);
-                if (has_b) b[k].raw = *reinterpret_cast<const uint4 *>(src + at_b);
+                a[k].raw = load16<kStream>(src + at_a);
+                if (has_b) b[k].raw = load16<kStream>(src + at_b);
             }
             h += S.step;
         }
@@ -233,27 +251,26 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowS
             if (out != nullptr) {
                 out += (token0 + token[k]) * (of_k < 0 ? A.q_out.token_stride : A.k_out.token_stride) +
                        (of_k < 0 ? h * A.q_out.head_stride : of_k * A.k_out.head_stride);
-                *reinterpret_cast<uint4 *>(out + at_a) = a[k].raw;
-                if (has_b) *reinterpret_cast<uint4 *>(out + at_b) = b[k].raw;
+                store16<kStream>(out + at_a, a[k].raw);
+                if (has_b) store16<kStream>(out + at_b, b[k].raw);
             }
         }
         if (store && of_k >= 0) {
             const int64_t at = place_in_cache[token[k]];
             if (at >= 0) {
                 T *out = (T *)(of_v < 0 ? A.k_cache : A.v_cache) + at + (of_v < 0 ? of_k : of_v) * A.cache_head_stride;
-                *reinterpret_cast<uint4 *>(out + at_a) = a[k].raw;
-                if (has_b) *reinterpret_cast<uint4 *>(out + at_b) = b[k].raw;
+                store16<kStream>(out + at_a, a[k].raw);
+                if (has_b) store16<kStream>(out + at_b, b[k].raw);
             }
         }
     }
 }
 
-// Whether all rows of a call can be read and written 16 bytes at a time, pairs whole.
-bool rows_aligned(const prep_rotary &R, const prep_rotary_args &A)
+// Whether all rows of a call start at multiples of `bytes`.
+bool rows_aligned(const prep_rotary &R, const prep_rotary_args &A, int64_t bytes)
 {
-    const int64_t v = 16 / element_bytes(R.dtype);
-    if (R.head_dim % v != 0 || (R.pairing == PREP_PAIR_HALVES ? R.pairs : 2 * R.pairs) % v != 0) return false;
-    auto fits = [&](const void *p, int64_t s, int64_t t) { return aligned(p, 16) && s % v == 0 && t % v == 0; };
+    const int64_t v = bytes / element_bytes(R.dtype);
+    auto fits = [&](const void *p, int64_t s, int64_t t) { return aligned(p, (uintptr_t)bytes) && s % v == 0 && t % v == 0; };
     auto rows = [&](const prep_heads &x) { return x.data == nullptr || fits(x.data, x.token_stride, x.head_stride); };
     if (A.q_heads > 0 && !(rows(A.q) && rows(A.q_out))) return false;
     if (A.k_heads > 0 && !(rows(A.k) && rows(A.k_out))) return false;
@@ -261,8 +278,17 @@ bool rows_aligned(const prep_rotary &R, const prep_rotary_args &A)
         return rows(A.v) && fits(A.k_cache, A.block_stride, A.slot_stride) && fits(A.v_cache, A.cache_head_stride, 0);
     return true;
 }
+// Whether all rows can be read and written 16 bytes at a time, pairs whole.
+bool rows_in_16(const prep_rotary &R, const prep_rotary_args &A)
+{
+    const int64_t v = 16 / element_bytes(R.dtype);
+    return R.head_dim % v == 0 && (R.pairing == PREP_PAIR_HALVES ? R.pairs : 2 * R.pairs) % v == 0 && rows_aligned(R, A, 16);
+}
 
-constexpr int kManyRows = 4;  // rows of a lane in large calls
+// Rows of a lane in large calls, from some two rounds of a full chip on.  Passes over fresh data, us, with 1, 2, 4, 8 rows: 8192
+// tokens of 28 + 4 heads of 128 in bf16 into the cache 36, 34, 36, 39; 19321 of 16 + 16 of 80 in fp16 in a fused projection
+// 43, 44, 49, 52; 16384 of 32 + 8 of 64 in fp32 63, 64, 67, 71.
+constexpr int kManyRows = 2;
 
 template <typename T, bool kHalves>
 int launch_rows(const prep_rotary &R, const prep_rotary_args &A, hipStream_t stream)
@@ -283,11 +309,16 @@ int launch_rows(const prep_rotary &R, const prep_rotary_args &A, hipStream_t str
     S.tokens = tokens_of(S.step * per_lane);
     const int64_t blocks = (S.rows + S.step * per_lane - 1) / (S.step * per_lane);
     if (blocks > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
+    // Past the caches where what a load takes of a row is whole 128-byte lines: then 34 -> 30 us and 64 -> 58 us (the first and the last
+    // of the calls above), 35 -> 29 for rows of 256 in bf16; pieces of 64 bytes 34 -> 34, of 80 and 96 bytes 44 -> 55 and 35 -> 39.
+    const bool lines = S.units * 16 % 128 == 0 && rows_aligned(R, A, 128);
     const dim3 grid((uint32_t)blocks);
     if (per_lane == 1)
-        hipLaunchKernelGGL((rotary_rows<T, kHalves, 1>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+        hipLaunchKernelGGL((rotary_rows<T, kHalves, 1, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    else if (!lines)
+        hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
     else
-        hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+        hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
     return PREP_OK;
 }
 
@@ -295,7 +326,7 @@ template <typename T>
 int launch_for(const prep_rotary &R, const prep_rotary_args &A, hipStream_t stream)
 {
     const bool halves = R.pairing == PREP_PAIR_HALVES;
-    if (rows_aligned(R, A)) return halves ? launch_rows<T, true>(R, A, stream) : launch_rows<T, false>(R, A, stream);
+    if (rows_in_16(R, A)) return halves ? launch_rows<T, true>(R, A, stream) : launch_rows<T, false>(R, A, stream);
     RotaryShape S;
     S.head_dim = R.head_dim;
     S.pairs = R.pairs;

@@ -30,6 +30,8 @@ inline int __clz(int v) { return v == 0 ? 32 : __builtin_clz((unsigned)v); }
 
 inline hipError_t hipGetDevice(int *d) { *d = 0; return hipSuccess; }
 
+#define __builtin_nontemporal_load(p) (*(p))
+#define __builtin_nontemporal_store(v, p) (*(p) = (v))
 #define __builtin_amdgcn_fence(...) ((void)0)
 // all lanes of the wave come here
 inline void __builtin_amdgcn_wave_barrier()
