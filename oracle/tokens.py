@@ -57,8 +57,7 @@ def patch_rows(frames, out_h, out_w, patch, merge, group, antialias, mean, std):
     """frames uint8 [f, h, w, 3] -> float64 [rows, 3 * group * patch * patch]."""
     f, h, w, _ = frames.shape
     wy, wx = axis_weights(h, out_h, antialias), axis_weights(w, out_w, antialias)
-    v = np.einsum("yh,fhwc->fywc", wy, frames.astype(np.float64))
-    v = np.einsum("xw,fywc->fyxc", wx, v)
+    v = np.stack([np.stack([wy @ frame[..., c].astype(np.float64) @ wx.T for c in range(3)], -1) for frame in frames])
     v = (v / 255.0 - np.asarray(mean, dtype=np.float64)) / np.asarray(std, dtype=np.float64)
     rows = []
     for t in range(-(-f // group)):

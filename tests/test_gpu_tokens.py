@@ -51,6 +51,16 @@ def test_patch_rows(backend, name):
     cases.check_patches(backend, name, seed=1, out_pad=0, pitch_pad=0, lead=0)
 
 
+@pytest.mark.parametrize("name", cases.PATCHES_LARGE)
+def test_many_patch_rows(backend, name):
+    cases.check_patches(backend, name)
+
+
+@pytest.mark.parametrize("name", cases.ROTARY_LARGE)
+def test_many_rotated_rows(backend, name):
+    cases.check_rotary(backend, name)
+
+
 @pytest.mark.parametrize("name", cases.POSITIONS)
 def test_places(backend, name):
     cases.check_positions(backend, name)

@@ -64,6 +64,16 @@ PATCHES = {
 }
 
 
+# more tiles than a GPU holds at a time, so that workgroups take several
+PATCHES_LARGE = {
+    "large_photos": ([(640, 480), (333, 517), (500, 375)] * 4, [1] * 12, 14, 2, 2, "bf16", True, 0, 0),
+    "large_clip": ([(900, 700)], [7], 14, 2, 2, "f16", True, 0, 400 * 300),
+    "large_parts": ([(900, 700)], [3], 40, 1, 1, "bf16", True, 0, 0),
+    "large_two_taps": ([(640, 480)] * 70, [1] * 70, 16, 1, 1, "f32", False, 0, 300 * 300),
+    "large_strong": ([(1500, 1200)], [2], 7, 2, 1, "f32", True, 0, 250 * 200),
+}
+
+
 def picture(rng, shape):
     """Noise, flat stretches and the extremes."""
     v = rng.integers(0, 256, shape)
@@ -88,7 +98,7 @@ def patch_tolerance(w, h, out_w, out_h, antialias):
 
 
 def check_patches(backend, name, seed=0, out_pad=3, pitch_pad=4, lead=5):
-    sizes, frames, patch, merge, group, dtype, antialias, least, most = PATCHES[name]
+    sizes, frames, patch, merge, group, dtype, antialias, least, most = (PATCHES | PATCHES_LARGE)[name]
     rng = np.random.default_rng(seed)
     params = prep.make_patch_params(patch, merge, group, dtype, MEAN, STD, prep.FILTER_ANTIALIAS if antialias else prep.FILTER_BILINEAR,
                                     min_pixels=least, max_pixels=most)
@@ -279,6 +289,14 @@ ROTARY = {
     "store_only_keys": (6, 0, 2, 64, (32, 0, 0), "f16", False, False, False, 1e4, 400, "fused", "store"),
     "many_heads": (5, 33, 7, 24, (12, 0, 0), "bf16", False, False, False, 1e4, 400, "plain", ""),
 }
+# calls of many rows (a GPU's)
+ROTARY_LARGE = {
+    "large_lines": (2100, 14, 2, 128, (16, 24, 24), "bf16", False, False, False, 1e6, 30000, "fused", "store"),
+    "large_lines_f32": (3000, 9, 3, 64, (12, 10, 10), "f32", True, True, False, 1e4, 5000, "plain", "inverse"),
+    "large_pieces": (3001, 8, 8, 80, (0, 20, 20), "f16", False, False, True, 1e4, 140, "fused", ""),
+    "large_in_place": (2500, 14, 2, 128, (64, 0, 0), "f16", False, False, False, 1e4, 9000, "fused", "in_place"),
+    "large_pairs": (700, 5, 2, 50, (9, 8, 8), "bf16", True, False, False, 1e4, 9000, "plain", ""),
+}
 # |error of cos or sin|: the angle is an eighth of a turn at most, rounded twice (as a float, times 2 pi / 2^32) and cut at 2^-33 of a
 # turn; the series' remainder; its evaluation, two roundings of values up to 1 that count in full (the others are scaled by x^2 / 2 < 0.31)
 TRIG = (math.pi / 4) * 2 * ULP + 2 * math.pi * 2.0 ** -33 + 2e-9 + 3 * ULP
@@ -328,7 +346,7 @@ class Laid:
 
 
 def check_rotary(backend, name, seed=0):
-    n, qh, kh, d, sections, dtype, adjacent, interleaved, per_axis, base, reach, layout, what = ROTARY[name]
+    n, qh, kh, d, sections, dtype, adjacent, interleaved, per_axis, base, reach, layout, what = (ROTARY | ROTARY_LARGE)[name]
     rng = np.random.default_rng(seed + 11)
     inverse, store = "inverse" in what, "store" in what
     low, high = sorted((0, reach))
