@@ -512,7 +512,8 @@ typedef struct {
  *   next          DEVICE  n_seq entries, or NULL: the place of the token that would follow each sequence
  *   workspace     DEVICE  16-byte aligned, at least prep_token_positions_workspace(n_segments) bytes, of this call
  *                 alone until it has run
- * Places are computed modulo 2^32.  n_seq <= 65535.
+ * Places are computed modulo 2^32.  n_seq <= 65535.  What is written must not overlap what is read (next is not
+ * first: a caller that goes on from next swaps the two).
  */
 uint64_t prep_token_positions_workspace(int32_t n_segments);
 int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n_segments, const int32_t *seq_segments,
@@ -597,13 +598,13 @@ typedef struct {
 } prep_heads;
 
 typedef struct {
-    int64_t n_tokens;          /* >= 0                                              */
+    int64_t n_tokens;          /* 0..2^31 - 1                                       */
     const int32_t *positions;  /* DEVICE: axis a of token i at [a * axis_stride + i] */
     int64_t axis_stride;
     prep_heads q, q_out;       /* q_heads heads, rotated from q to q_out            */
     prep_heads k, k_out;       /* k_heads heads; k_out.data may be NULL with a cache */
     prep_heads v;              /* k_heads heads, copied into the cache              */
-    int32_t q_heads, k_heads;  /* >= 0 each, not both 0                             */
+    int32_t q_heads, k_heads;  /* 0..65535 each, not both 0                         */
     int32_t inverse;           /* 1: rotate by -u, which is also the way back: the gradient with respect to
                                   the input, given the one with respect to the output */
     int32_t block_size;

@@ -1,4 +1,5 @@
-"""MI355X-native batched JPEG -> model-input tensor preprocessing.
+"""MI355X-native batched JPEG -> model-input tensor preprocessing, and the inputs of language models
+that read images and video: patch rows, places of tokens, rotary embedding, cache slots.
 
 Thin ctypes binding of ``libprep.so`` (the C ABI declared in ``include/prep.h``).
 All work happens in the library's HIP kernels; this module only marshals

@@ -508,7 +508,8 @@ int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n
 {
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     if (n_segments < 0 || n_segments > kMaxEntries || n_seq < 0 || n_seq > 65535 || merge < 1 || merge > 32767 || capacity < 0 ||
-        capacity > 0x7FFFFFFF || (n_segments > 0 && !segments) || !seq_segments || (capacity > 0 && !positions) || !token_starts || !workspace)
+        capacity > 0x7FFFFFFF || (n_segments > 0 && !segments) || !seq_segments || (capacity > 0 && !positions) || !token_starts || !workspace ||
+        (next && next == first) || token_starts == seq_segments || (const void *)token_starts == (const void *)first)
         return PREP_E_INVALID_ARG;
     if (!aligned(segments, 4) || !aligned(seq_segments, 4) || !aligned(first, 4) || !aligned(positions, 4) || !aligned(token_starts, 4) ||
         !aligned(next, 4) || !aligned(workspace, 16))

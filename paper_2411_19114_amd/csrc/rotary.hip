@@ -183,13 +183,10 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowS
     Vec<T> a[kRows], b[kRows];
     int token[kRows], head[kRows];  // of the rows; token -1: none
     {
-        int t = 0, h = head0 + lane_row;
+        const int step_t = S.step / S.heads, step_h = S.step - step_t * S.heads;
+        int t = (head0 + lane_row) / S.heads, h = head0 + lane_row - t * S.heads;
 #pragma unroll
         for (int k = 0; k < kRows; k++) {
-            while (h >= S.heads) {
-                h -= S.heads;
-                t++;
-            }
             const bool mine = works && row0 + lane_row + k * S.step < S.rows;
             token[k] = mine ? t : -1;
             head[k] = h;
@@ -202,7 +199,12 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowS
                 a[k].raw = load16<kStream>(src + at_a);
                 if (has_b) b[k].raw = load16<kStream>(src + at_b);
             }
-            h += S.step;
+            t += step_t;
+            h += step_h;
+            if (h >= S.heads) {
+                h -= S.heads;
+                t++;
+            }
         }
     }
     const int n = (int)min((int64_t)S.tokens, A.n_tokens - token0);
@@ -451,7 +453,7 @@ int prep_rotary_apply(prep_rotary *r, const prep_rotary_args *args, void *stream
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     if (!r || !args) return PREP_E_INVALID_ARG;
     prep_rotary_args A = *args;
-    if (A.n_tokens < 0 || A.q_heads < 0 || A.k_heads < 0 || A.q_heads > 65535 || A.k_heads > 65535 || A.q_heads + A.k_heads == 0 ||
+    if (A.n_tokens < 0 || A.n_tokens > 0x7FFFFFFF || A.q_heads < 0 || A.k_heads < 0 || A.q_heads > 65535 || A.k_heads > 65535 || A.q_heads + A.k_heads == 0 ||
         A.axis_stride < 0 || (A.inverse != 0 && A.inverse != 1))
         return PREP_E_INVALID_ARG;
     const bool store = A.k_cache != nullptr;

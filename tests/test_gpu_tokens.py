@@ -92,6 +92,52 @@ def test_refusals(backend):
     cases.check_rotary_refusals(backend)
 
 
+def test_a_device_that_is_not_there(backend):
+    """An error, and the current device and the calls after it are as before."""
+    torch = backend.torch
+    x = torch.zeros(4096, dtype=torch.int64, device="cuda")
+    p = x.data_ptr()
+    params = prep.make_patch_params(4, 1, 1, "f32", cases.MEAN, cases.STD)
+    cases.refused(prep.E_HIP, prep.patch_rows, 99, p, [0], [4], [4], [12], params, p + 4096, 10)
+    cases.refused(prep.E_HIP, prep.token_positions, p, 1, p, 1, 0, 1, p + 4096, 8, p + 8192, 0, p + 16384, 1024, device=99)
+    cases.refused(prep.E_HIP, prep.block_slots, 1, 4, 9, p, p + 64, p + 128, 4, p + 256, p + 512, 4, 4, p + 1024, 8, p + 2048, p + 2304, p + 2560, p + 2816,
+                  p + 4096, 1024, device=99)
+    assert torch.cuda.current_device() == 0
+    torch.cuda.synchronize()
+    cases.check_slots(backend, "step")
+
+
+def test_two_streams_at_once(backend):
+    """Calls that overlap on two streams, each with its own outputs and one rotary handle between them."""
+    torch = backend.torch
+    rng = np.random.default_rng(6)
+    rotary = prep.Rotary(64, (16, 8, 8), 1e4, "f32")
+    n, h = 4000, 4
+    positions = rng.integers(0, 5000, (3, n)).astype(np.int32)
+    x = [rng.standard_normal((n, h, 64)).astype(np.float32) for _ in range(2)]
+    image = rng.integers(0, 256, (1, 300, 400, 3)).astype(np.uint8)
+    params = prep.make_patch_params(16, 2, 1, "f32", cases.MEAN, cases.STD)
+    places, src = torch.from_numpy(positions).cuda(), torch.from_numpy(image.reshape(-1)).cuda()
+    given, out = [torch.from_numpy(v).cuda() for v in x], [torch.zeros((n, h, 64), device="cuda") for _ in range(2)]
+    grid = prep.patch_grid(params, 400, 300)
+    rows = grid[1] * grid[2]
+    pixels = [torch.zeros((rows, 768), device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            rotary.apply(n, places.data_ptr(), n, q=(given[i].data_ptr(), h * 64, 64), q_out=(out[i].data_ptr(), h * 64, 64), q_heads=h, stream=s.cuda_stream)
+            prep.patch_rows(0, src.data_ptr(), [0], [400], [300], [1200], params, pixels[i].data_ptr(), rows, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    axes, freqs = oracle.pair_axes((16, 8, 8), False), oracle.frequencies((16, 8, 8), 1e4, False, False)
+    want_rows = oracle.patch_rows(image, grid[1] * 16, grid[2] * 16, 16, 2, 1, False, cases.MEAN, cases.STD)
+    for i in range(2):
+        v = x[i].astype(np.float64)
+        cases.within(out[i].cpu().double().numpy(), oracle.rotary(v, positions, axes, freqs, False, False), cases.rotary_tolerance(v, 32, False), "f32")
+        cases.within(pixels[i].cpu().double().numpy(), want_rows, cases.patch_tolerance(400, 300, grid[2] * 16, grid[1] * 16, False), "f32")
+    rotary.close()
+
+
 def test_another_stream(backend):
     """Work goes to the stream that is named, whatever the current one."""
     torch = backend.torch

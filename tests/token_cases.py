@@ -287,10 +287,12 @@ ROTARY = {
     "store_partial": (9, 1, 1, 80, (12, 0, 0), "bf16", False, False, False, 1e4, 400, "fused", "store"),
     "store_one": (1, 8, 1, 128, (64, 0, 0), "bf16", False, False, False, 1e4, 400, "fused", "store"),
     "store_only_keys": (6, 0, 2, 64, (32, 0, 0), "f16", False, False, False, 1e4, 400, "fused", "store"),
+    "one_head": (300, 1, 0, 32, (16, 0, 0), "bf16", False, False, False, 1e4, 400, "plain", ""),
     "many_heads": (5, 33, 7, 24, (12, 0, 0), "bf16", False, False, False, 1e4, 400, "plain", ""),
 }
 # calls of many rows (a GPU's)
 ROTARY_LARGE = {
+    "large_one_head": (40000, 1, 1, 32, (16, 0, 0), "bf16", False, False, False, 1e4, 400, "plain", ""),
     "large_lines": (2100, 14, 2, 128, (16, 24, 24), "bf16", False, False, False, 1e6, 30000, "fused", "store"),
     "large_lines_f32": (3000, 9, 3, 64, (12, 10, 10), "f32", True, True, False, 1e4, 5000, "plain", "inverse"),
     "large_pieces": (3001, 8, 8, 80, (0, 20, 20), "f16", False, False, True, 1e4, 140, "fused", ""),
@@ -520,7 +522,7 @@ def check_packing_refusals(backend):
     for kw in (dict(n_segments=-1), dict(n_segments=(1 << 20) + 1), dict(n_seq=-1), dict(n_seq=65536), dict(merge=0), dict(merge=32768),
                dict(capacity=-1), dict(capacity=2 ** 31), dict(segments_ptr=0), dict(seq_segments_ptr=0), dict(positions_ptr=0),
                dict(token_starts_ptr=0), dict(workspace_ptr=0), dict(segments_ptr=p + 2), dict(positions_ptr=p + 1), dict(first_ptr=p + 3),
-               dict(next_ptr=p + 2), dict(workspace_ptr=p + 8), dict(token_starts_ptr=p + 1), dict(seq_segments_ptr=p + 1)):
+               dict(next_ptr=p + 2), dict(first_ptr=p + 64, next_ptr=p + 64), dict(token_starts_ptr=p), dict(workspace_ptr=p + 8), dict(token_starts_ptr=p + 1), dict(seq_segments_ptr=p + 1)):
         refused(E, prep.token_positions, **{**good, **kw})
     refused(L, prep.token_positions, **{**good, "workspace_bytes": prep.token_positions_workspace(2) - 1})
     assert prep.token_positions_workspace(-1) == 0 and prep.token_positions_workspace((1 << 20) + 1) == 0
@@ -556,7 +558,7 @@ def check_rotary_refusals(backend):
                 k_out=(p + 8192, 16, 16), k_heads=1, stream=backend.stream)
     cache = dict(v=(p + 3072, 16, 16), k_cache=p + 12288, v_cache=p + 16384, n_blocks=2, block_size=2, block_stride=32, slot_stride=16,
                  cache_head_stride=16, slots=p + 20480)
-    bad = [dict(n_tokens=-1), dict(positions=0), dict(positions=p + 2), dict(axis_stride=-1), dict(q_heads=-1), dict(k_heads=-1),
+    bad = [dict(n_tokens=-1), dict(n_tokens=2 ** 31), dict(q_heads=65536), dict(positions=0), dict(positions=p + 2), dict(axis_stride=-1), dict(q_heads=-1), dict(k_heads=-1),
            dict(q_heads=0, k_heads=0), dict(q=(0, 32, 16)), dict(q_out=(0, 32, 16)), dict(q=(p + 2, 32, 16)), dict(q_out=(p + 4098, 32, 16)),
            dict(q=(p + 1024, -32, 16)), dict(q_out=(p + 4096, 32, 0)), dict(q_out=(p + 4096, 16, 16)), dict(q_out=(p + 4096, 32, 8)),
            dict(q_out=(p + 1024, 64, 16)), dict(k_out=(0, 0, 0)), dict(k_out=(p + 8192, 0, 16))]
