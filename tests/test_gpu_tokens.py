@@ -271,6 +271,48 @@ def test_captured_calls_follow_their_lengths(backend):
     rotary.close()
 
 
+def test_captured_patch_rows_and_backward_rotation(backend):
+    """One graph of both, replayed on new contents of the same buffers with eager work between, against the oracle and an eager call."""
+    torch = backend.torch
+    rng = np.random.default_rng(9)
+    w, h, n, heads, d = 200, 150, 300, 3, 64
+    params = prep.make_patch_params(14, 2, 2, "f32", cases.MEAN, cases.STD, prep.FILTER_ANTIALIAS, max_pixels=120 * 120)
+    grid = prep.patch_grid(params, w, h, 3)
+    rows = grid[0] * grid[1] * grid[2]
+    src = torch.zeros(3 * h * w * 3, dtype=torch.uint8, device="cuda")
+    pixels, gradient, out = torch.zeros((rows, 1176), device="cuda"), torch.zeros((n, heads, d), device="cuda"), torch.zeros((n, heads, d), device="cuda")
+    places = torch.zeros((3, n), dtype=torch.int32, device="cuda")
+    rotary = prep.Rotary(d, (12, 10, 10), 1e4, "f32")
+
+    def both(pixels, out):
+        s = torch.cuda.current_stream().cuda_stream
+        prep.patch_rows(0, src.data_ptr(), [0], [w], [h], [3 * w], params, pixels.data_ptr(), rows, frames=[3], frame_strides=[3 * w * h], stream=s)
+        rotary.apply(n, places.data_ptr(), n, q=(gradient.data_ptr(), heads * d, d), q_out=(out.data_ptr(), heads * d, d), q_heads=heads, inverse=True, stream=s)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(pixels, out)
+    axes, freqs = oracle.pair_axes((12, 10, 10), False), oracle.frequencies((12, 10, 10), 1e4, False, False)
+    for _ in range(4):
+        clip = cases.picture(rng, (3, h, w, 3))
+        g = rng.standard_normal((n, heads, d)).astype(np.float32)
+        p = rng.integers(0, 9000, (3, n)).astype(np.int32)
+        src.copy_(torch.from_numpy(clip.reshape(-1)))
+        gradient.copy_(torch.from_numpy(g))
+        places.copy_(torch.from_numpy(p))
+        graph.replay()
+        eager = torch.zeros_like(pixels), torch.zeros_like(out)
+        both(*eager)
+        torch.cuda.synchronize()
+        assert torch.equal(eager[0], pixels) and torch.equal(eager[1], out)
+        want = oracle.patch_rows(clip, grid[1] * 14, grid[2] * 14, 14, 2, 2, True, cases.MEAN, cases.STD)
+        cases.within(pixels.cpu().double().numpy(), want, cases.patch_tolerance(w, h, grid[2] * 14, grid[1] * 14, True), "f32")
+        v = g.astype(np.float64)
+        cases.within(out.cpu().double().numpy(), oracle.rotary(v, p, axes, freqs, False, True), cases.rotary_tolerance(v, 32, False), "f32")
+    rotary.close()
+
+
 def test_from_files_to_the_cache(backend):
     """A step of a model that reads pictures, without the model: files to patch rows, the encoder's places and rotation, then the places,
     slots and rotation into the cache of prompts that hold the pictures' merged tokens."""
