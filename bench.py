@@ -693,6 +693,7 @@ def main():
 
     def leg(host_input):
         """W untimed steps, then exactly K timed ones between two device synchronisations."""
+        turn[0] = 0   # the handles asked below are those that took these steps
         for _ in range(args.warmup):
             step(host_input)
         torch.cuda.synchronize()
@@ -740,7 +741,7 @@ def main():
         in_turn[0] = n_handles
         overlapped = {"streams": overlap, "input": "resident in HBM", "value": n * args.steps / o_wall,
                       "unit": "images/s", "steps": args.steps, "ms_per_step": o_wall / args.steps * 1e3}
-        for h in pps[:overlap]:
+        for h in pps[:min(overlap, args.steps)]:
             assert h.get_status(n) == [0] * n
 
     # S1 alone: the time inside the entry point (marker/table parsing, launch planning,
