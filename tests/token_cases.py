@@ -556,7 +556,7 @@ def check_rotary_refusals(backend):
     n = 3
     good = dict(n_tokens=n, positions=p, axis_stride=n, q=(p + 1024, 32, 16), q_out=(p + 4096, 32, 16), q_heads=2, k=(p + 2048, 16, 16),
                 k_out=(p + 8192, 16, 16), k_heads=1, stream=backend.stream)
-    cache = dict(v=(p + 3072, 16, 16), k_cache=p + 12288, v_cache=p + 16384, n_blocks=2, block_size=2, block_stride=32, slot_stride=16,
+    cache = dict(v=(p + 2560, 16, 16), k_cache=p + 12288, v_cache=p + 16384, n_blocks=2, block_size=2, block_stride=32, slot_stride=16,
                  cache_head_stride=16, slots=p + 20480)
     bad = [dict(n_tokens=-1), dict(n_tokens=2 ** 31), dict(q_heads=65536), dict(positions=0), dict(positions=p + 2), dict(axis_stride=-1), dict(q_heads=-1), dict(k_heads=-1),
            dict(q_heads=0, k_heads=0), dict(q=(0, 32, 16)), dict(q_out=(0, 32, 16)), dict(q=(p + 2, 32, 16)), dict(q_out=(p + 4098, 32, 16)),
