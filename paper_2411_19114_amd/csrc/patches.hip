@@ -492,23 +492,24 @@ __global__ __launch_bounds__(kThreads) void patch_rows_direct(const uint8_t *__r
 {
     const int clip = clip_of(pack, blockIdx.x);
     const PatchClip &C = pack.c[clip];
-    const int area = g.patch * g.patch;
-    const int cols = C.cols, rows = C.rows;
-    const int64_t per_frame = (int64_t)cols * rows * area;
+    // (a frame's pixels and rows are below 2^32, sides being at most 65535, but not below 2^31)
+    const uint32_t area = (uint32_t)(g.patch * g.patch), cols = C.cols, rows = C.rows, merge = (uint32_t)g.merge;
+    const int64_t per_frame = (int64_t)(cols * rows * area);
     const int64_t item = (int64_t)(blockIdx.x - pack.block0[clip]) * kThreads + threadIdx.x;
-    const int groups = (C.frames - 1) / g.group + 1;
+    const int64_t groups = (C.frames - 1) / g.group + 1;
     if (item >= per_frame * g.group * groups) return;
-    const int slot = (int)(item / per_frame), e = (int)(item - slot * per_frame);
-    const int f = min(slot, C.frames - 1);
-    const int row = e / area, in_patch = e - row * area;  // row of the group
-    const int band = row / (g.merge * cols), r1 = row - band * g.merge * cols;
-    const int window = r1 / (g.merge * g.merge), r2 = r1 - window * g.merge * g.merge;
-    const int py = band * g.merge + r2 / g.merge, px = window * g.merge + r2 % g.merge;
-    const int y = py * g.patch + in_patch / g.patch, x = px * g.patch + in_patch % g.patch;
+    const int64_t slot = item / per_frame;
+    const uint32_t e = (uint32_t)(item - slot * per_frame);
+    const int64_t f = min(slot, (int64_t)C.frames - 1);
+    const uint32_t row = e / area, in_patch = e - row * area;  // row of the group
+    const uint32_t band = row / (merge * cols), r1 = row - band * merge * cols;
+    const uint32_t window = r1 / (merge * merge), r2 = r1 - window * merge * merge;
+    const uint32_t py = band * merge + r2 / merge, px = window * merge + r2 % merge;
+    const int y = (int)(py * (uint32_t)g.patch + in_patch / (uint32_t)g.patch), x = (int)(px * (uint32_t)g.patch + in_patch % (uint32_t)g.patch);
     float v[3] = {0.0f, 0.0f, 0.0f};
     if (status == nullptr || status[C.image] == PREP_OK) {
-        const float inv_y = g.antialias ? fminf((float)(rows * g.patch) / (float)C.height, 1.0f) : 1.0f;
-        const float inv_x = g.antialias ? fminf((float)(cols * g.patch) / (float)C.width, 1.0f) : 1.0f;
+        const float inv_y = g.antialias ? fminf((float)(C.rows * g.patch) / (float)C.height, 1.0f) : 1.0f;
+        const float inv_x = g.antialias ? fminf((float)(C.cols * g.patch) / (float)C.width, 1.0f) : 1.0f;
         const Taps ty = make_taps(y, C.height, C.scale_y(g.patch), inv_y, g.antialias), tx = make_taps(x, C.width, C.scale_x(g.patch), inv_x, g.antialias);
         const uint8_t *src = rgb + C.src_off + (uint64_t)f * C.frame_stride;
         float sum_x = 0.0f, sum_y = 0.0f;
@@ -530,7 +531,7 @@ __global__ __launch_bounds__(kThreads) void patch_rows_direct(const uint8_t *__r
 #pragma unroll
         for (int c = 0; c < 3; c++) v[c] = fmaf(v[c] * norm, g.scale[c], g.bias[c]);
     }
-    T *o = out + (C.row0 + (int64_t)(slot / g.group) * rows * cols + row) * out_stride + (int64_t)(slot % g.group) * area + in_patch;
+    T *o = out + (C.row0 + slot / g.group * (int64_t)(rows * cols) + row) * out_stride + slot % g.group * (int64_t)area + in_patch;
 #pragma unroll
     for (int c = 0; c < 3; c++) o[(int64_t)c * g.group * area] = from_float<T>(v[c]);
 }

@@ -1,0 +1,107 @@
+"""Calls of the operators for packed batches of tokens whose sizes come near what 32 bits hold, without a GPU: their sources compiled by
+g++, a few workgroups of each launch run on buffers of address space of which few pages are touched."""
+import ctypes as C
+import mmap
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+import emul
+import paper_2411_19114_amd.binding as prep
+import token_cases as cases
+from oracle import tokens as oracle
+
+
+class Library:
+    def __init__(self, path):
+        self.lib = C.CDLL(path)
+
+    def want(self, groups=()):
+        self.lib.some_workgroups_want((C.c_uint64 * len(groups))(*groups), len(groups))
+
+    def launches(self):
+        """(workgroups before it, workgroups, threads) of each launch since want()."""
+        out, got = (C.c_uint64 * 3)(), []
+        for i in range(self.lib.some_workgroups_launch(1 << 30, out)):
+            self.lib.some_workgroups_launch(i, out)
+            got.append(tuple(out))
+        return got
+
+
+def _build(where, source, rest=""):
+    path = str(where / (source + ".so"))
+    (where / (source + ".cpp")).write_text(f'#include "some_workgroups.h"\n#include "{os.path.join(emul.CSRC, source)}"\n{rest}\n')
+    subprocess.run(["g++", "-std=c++20", "-O1", "-pthread", "-fPIC", "-shared", "-I", emul.EMU, "-I", emul.CSRC, "-include",
+                    os.path.join(emul.EMU, "more_hip.h"), str(where / (source + ".cpp")), "-o", path], check=True)
+    return Library(path)
+
+
+@pytest.fixture(scope="module")
+def patches(tmp_path_factory):
+    return _build(tmp_path_factory.mktemp("patches"), "patches.hip", "int prep::decode_batch(prep_handle *, const uint8_t *, const uint8_t *, const "
+                  "uint64_t *, int32_t, OutputStage *, hipStream_t) { return PREP_E_INVALID_ARG; }")
+
+
+class Sparse:
+    """Zeros, of which only what is touched takes memory."""
+
+    def __init__(self, size):
+        self.map = mmap.mmap(-1, size, flags=mmap.MAP_PRIVATE | mmap.MAP_ANONYMOUS | 0x4000)  # MAP_NORESERVE
+        self.bytes = np.frombuffer(self.map, dtype=np.uint8)
+        self.ptr = self.bytes.ctypes.data
+
+
+def _patch_rows(library, params, src, w, h, pitch, out, rows):
+    starts = (C.c_int64 * 2)()
+    rc = library.lib.prep_patch_rows(0, C.c_void_p(src), prep._packed("Q", [0]), prep._packed("i", [w]), prep._packed("i", [h]), prep._packed("i", [pitch]),
+                                     None, None, 1, C.byref(params), C.c_void_p(out), C.c_int64(0), C.c_int64(rows), starts, None)
+    return rc, list(starts)
+
+
+def place_of_row(row, cols, merge):
+    """(line, column) of patches of row `row` of a frame whose lines of patches come in windows of merge x merge."""
+    band, r = divmod(row, merge * cols)
+    window, r = divmod(r, merge * merge)
+    return band * merge + r // merge, window * merge + r % merge
+
+
+@pytest.mark.parametrize("side,merge", [(46368, 2), (65520, 5)])
+def test_frames_of_more_than_2_31_pixels(patches, side, merge):
+    """Rows of an enlarged still: those around pixel 2^31 of the rows' order, and the first and the last."""
+    w, patch = 16, 16
+    params = prep.make_patch_params(patch, merge, 1, "bf16", cases.MEAN, cases.STD, prep.FILTER_ANTIALIAS, min_pixels=side * side)
+    cols = side // patch
+    rows, area = cols * cols, patch * patch
+    assert rows * area > 2 ** 31
+    picture = cases.picture(np.random.default_rng(4), (w, w, 3))
+    # (as much room below the rows as a wrapped index reaches)
+    row_bytes = 3 * area * 2
+    below = 2 ** 31 * 6 + (1 << 20)
+    out = Sparse(below + rows * row_bytes)
+    looked_at = [0, 2 ** 31 // area - 1, 2 ** 31 // area, 2 ** 31 // area + 1, rows - 1]  # (256 pixels are a workgroup's and a row's)
+    patches.want(looked_at)
+    rc, starts = _patch_rows(patches, params, picture.ctypes.data, w, w, 3 * w, out.ptr + below, rows)
+    assert rc == 0 and starts == [0, rows]
+    weights = _enlarging_weights(w, side)
+    for row in looked_at:
+        y, x = place_of_row(row, cols, merge)
+        wy, wx = weights(range(y * patch, (y + 1) * patch)), weights(range(x * patch, (x + 1) * patch))
+        v = np.stack([wy @ picture[..., c].astype(np.float64) @ wx.T for c in range(3)])
+        want = ((v / 255 - np.array(cases.MEAN)[:, None, None]) / np.array(cases.STD)[:, None, None]).ravel()
+        at = below + row * row_bytes
+        got = cases.unpack(out.bytes[at:at + row_bytes].view(np.uint16), "bf16")
+        cases.within(got, want, cases.patch_tolerance(w, w, side, side, True), "bf16")
+
+
+def _enlarging_weights(size, out):
+    def rows(which):
+        m = np.zeros((len(which), size))
+        for k, i in enumerate(which):
+            centre = (i + 0.5) * size / out - 0.5
+            low = int(np.floor(centre))
+            m[k, min(max(low, 0), size - 1)] += 1 - (centre - low)
+            m[k, min(max(low + 1, 0), size - 1)] += centre - low
+        return m
+    return rows
