@@ -485,7 +485,7 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
 }
 
 // Any sizes: one thread produces the three channels of one pixel, pixels in the order of the rows.  For images narrower than a
-// tile's reads and reductions so strong that a tile's samples do not fit its LDS.
+// tile's reads, reductions so strong that a tile's samples do not fit its LDS, and what a tile's 32-bit offsets do not reach.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void patch_rows_direct(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
                                                               const int32_t *__restrict__ status, T *__restrict__ out, int64_t out_stride)
@@ -592,8 +592,8 @@ bool patch_size(const prep_patch_params *p, int32_t width, int32_t height, int32
 template <typename Most>
 bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
 {
-    // (offsets inside a frame group are 32-bit)
-    if (c->width < kNarrowest || (int64_t)c->cols * c->rows * out_stride > INT32_MAX) return false;
+    // (offsets inside a frame group are 32-bit, and so are those inside the samples under a tile)
+    if (c->width < kNarrowest || (int64_t)c->cols * c->rows * out_stride > INT32_MAX || (uint64_t)c->pitch * Most::source_rows > UINT32_MAX) return false;
     const double scale_x = c->scale_x(g.patch), scale_y = c->scale_y(g.patch);
     const double sx = g.antialias && scale_x > 1.0 ? scale_x : 1.0, sy = g.antialias && scale_y > 1.0 ? scale_y : 1.0;
     // Under n output samples in a row lie fewer than (n - 1) scale + 2 s + 1 source samples; columns come in sixteens.

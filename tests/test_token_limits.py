@@ -105,3 +105,22 @@ def _enlarging_weights(size, out):
             m[k, min(max(low + 1, 0), size - 1)] += centre - low
         return m
     return rows
+
+
+@pytest.mark.parametrize("h", [26, 70])
+@pytest.mark.parametrize("pitch", [3 * 40, 2 ** 26 + 128, 2 ** 27 + 64, 2 ** 30, 2 ** 31 - 1])
+def test_rows_far_apart(patches, pitch, h):
+    """Rows whose distance times the rows under a tile passes 32 bits."""
+    w, patch, most = 40, 13, 0 if h == 26 else 26 * 26  # (near the picture's size, or reduced, so that a tile has many rows)
+    params = prep.make_patch_params(patch, 1, 1, "f32", cases.MEAN, cases.STD, prep.FILTER_ANTIALIAS, max_pixels=most)
+    oh, ow = oracle.patch_size(w, h, patch, 1, 0, most)
+    picture = cases.picture(np.random.default_rng(5), (h, w, 3))
+    src = Sparse(pitch * (h - 1) + 3 * w)
+    for y in range(h):
+        src.bytes[y * pitch:y * pitch + 3 * w] = picture[y].ravel()
+    want = oracle.patch_rows(picture[None], oh, ow, patch, 1, 1, True, cases.MEAN, cases.STD)
+    out = np.zeros(want.shape, dtype=np.float32)
+    patches.want(range(64))
+    rc, starts = _patch_rows(patches, params, src.ptr, w, h, pitch, out.ctypes.data, len(want))
+    assert rc == 0 and starts == [0, len(want)] and patches.launches()[-1][0] + patches.launches()[-1][1] <= 64
+    cases.within(out.astype(np.float64), want, cases.patch_tolerance(w, h, ow, oh, True), "f32")
