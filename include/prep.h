@@ -620,7 +620,8 @@ typedef struct {
 int prep_rotary_create(prep_rotary **out, const prep_rotary_config *cfg);
 int prep_rotary_destroy(prep_rotary *r);
 /* Outputs may be their inputs (the same pointer and strides); apart from that, what is read and what
- * is written must not overlap.  A handle may be used by several threads and streams at once, and a call leaves nothing in it. */
+ * is written must not overlap.  A handle may be used by several threads and streams at once, and a call leaves nothing in it.
+ * PREP_E_TOO_LARGE, and nothing enqueued, beyond 2^31 - 1 workgroups (of some 8 KB of rows each). */
 int prep_rotary_apply(prep_rotary *r, const prep_rotary_args *args, void *stream);
 
 #ifdef __cplusplus

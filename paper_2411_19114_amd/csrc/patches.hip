@@ -92,6 +92,7 @@ struct PatchGeometry {
     int32_t antialias;
     int32_t strip;                // tiles of a workgroup
     int32_t chunk;                // bytes written at a time
+    uint32_t block0;              // first workgroup of the launch
     Divisor by_patch, by_merge, by_chunks;  // (chunks of a patch's channel)
     float scale[3], bias[3];      // 1 / (255 std), -mean / std
 };
@@ -248,12 +249,13 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
     __shared__ float col_centre[kTileCols], col_norm[kTileCols];
     __shared__ int32_t patch_row[2][kPatches], tile_down[kStrip], tile_part_rows[kStrip], tile_part_y0[kStrip];
 
-    const int clip = clip_of(pack, blockIdx.x);
+    const uint32_t block = g.block0 + blockIdx.x;
+    const int clip = clip_of(pack, block);
     const PatchClip &C = pack.c[clip];
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const int tiles_x = C.tiles_x(), tiles_y = C.tiles_y();
     const Divisor strips = {(uint32_t)(tiles_x * ((tiles_y + g.strip - 1) / g.strip)), C.strips_m}, strips_x = {(uint32_t)tiles_x, C.strips_x_m};
-    const uint32_t strip = blockIdx.x - pack.block0[clip], frames_group = strips.quotient(strip);
+    const uint32_t strip = block - pack.block0[clip], frames_group = strips.quotient(strip);
     const uint32_t in_group = strip - frames_group * strips.d, strip_y = strips_x.quotient(in_group);
     const int tile_x = (int)(in_group - strip_y * strips_x.d), tile_y0 = (int)strip_y * g.strip;
     const int tiles = min(g.strip, tiles_y - tile_y0);
@@ -490,12 +492,13 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void patch_rows_direct(const uint8_t *__restrict__ rgb, ClipPack pack, PatchGeometry g,
                                                               const int32_t *__restrict__ status, T *__restrict__ out, int64_t out_stride)
 {
-    const int clip = clip_of(pack, blockIdx.x);
+    const uint32_t block = g.block0 + blockIdx.x;
+    const int clip = clip_of(pack, block);
     const PatchClip &C = pack.c[clip];
     // (a frame's pixels and rows are below 2^32, sides being at most 65535, but not below 2^31)
     const uint32_t area = (uint32_t)(g.patch * g.patch), cols = C.cols, rows = C.rows, merge = (uint32_t)g.merge;
     const int64_t per_frame = (int64_t)(cols * rows * area);
-    const int64_t item = (int64_t)(blockIdx.x - pack.block0[clip]) * kThreads + threadIdx.x;
+    const int64_t item = (int64_t)(block - pack.block0[clip]) * kThreads + threadIdx.x;
     const int64_t groups = (C.frames - 1) / g.group + 1;
     if (item >= per_frame * g.group * groups) return;
     const int64_t slot = item / per_frame;
@@ -675,15 +678,17 @@ int chunk_bytes(const prep_patch_params *params, const PatchClip *clips, int32_t
 }
 
 template <typename T>
-void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, const PatchGeometry &g, int kind, const int32_t *status,
+void launch_for(const uint8_t *rgb, const ClipPack &pack, uint32_t blocks, PatchGeometry g, int kind, const int32_t *status,
                 T *out, int64_t out_stride, hipStream_t stream)
 {
-    if (kind == kWide)
-        hipLaunchKernelGGL((patch_rows_tiled<T, true>), dim3(blocks), dim3(Limits<true, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride);
-    else if (kind == kNarrow)
-        hipLaunchKernelGGL((patch_rows_tiled<T, false>), dim3(blocks), dim3(Limits<false, (int)sizeof(T)>::threads), 0, stream, rgb, pack, g, status, out, out_stride);
-    else
-        hipLaunchKernelGGL((patch_rows_direct<T>), dim3(blocks), dim3(kThreads), 0, stream, rgb, pack, g, status, out, out_stride);
+    const int threads = kind == kWide ? Limits<true, (int)sizeof(T)>::threads : kind == kNarrow ? Limits<false, (int)sizeof(T)>::threads : kThreads;
+    in_launches(blocks, threads, [&](uint32_t first, uint32_t n) {
+        const dim3 grid(n), block(threads);
+        g.block0 = first;
+        if (kind == kWide) hipLaunchKernelGGL((patch_rows_tiled<T, true>), grid, block, 0, stream, rgb, pack, g, status, out, out_stride);
+        else if (kind == kNarrow) hipLaunchKernelGGL((patch_rows_tiled<T, false>), grid, block, 0, stream, rgb, pack, g, status, out, out_stride);
+        else hipLaunchKernelGGL((patch_rows_direct<T>), grid, block, 0, stream, rgb, pack, g, status, out, out_stride);
+    });
 }
 
 // status: DEVICE, per PatchClip::image, or nullptr = all PREP_OK (others get rows of zeros).  clips, kinds: HOST, n of them; the tiles
@@ -692,6 +697,7 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int3
                       void *out, int64_t out_stride, hipStream_t stream)
 {
     PatchGeometry g;
+    g.block0 = 0;
     g.patch = params->patch;
     g.merge = params->merge;
     g.group = params->frames_per_patch;
@@ -784,7 +790,7 @@ public:
         skip_to(i);
         if (frames < 1 || !patch_size(params_, width, height, &rows, &cols)) return false;
         const int64_t groups = ((int64_t)frames - 1) / params_->frames_per_patch + 1;
-        // a launch has fewer than 2^31 workgroups
+        // fewer than 2^31 workgroups
         if (groups * params_->frames_per_patch * rows * cols * params_->patch * params_->patch > (int64_t)0x7FFFFFFF * kThreads) return false;
         PatchClip &c = clips_[count_++];
         c.src_off = src_off;

@@ -30,6 +30,7 @@ constexpr int kMaxTokens = 8;  // tokens of a workgroup
 struct RotaryShape {
     int32_t head_dim, pairs;
     int32_t tokens;  // of a workgroup
+    uint32_t block0;  // first workgroup of the launch
 };
 
 // cos and sin of a fraction of a turn.  Reduced to an eighth of a turn either side of a quadrant's middle
@@ -65,7 +66,7 @@ template <typename T, bool kHalves>
 __global__ __launch_bounds__(kThreads) void rotary_pairs(prep_rotary_args A, RotaryShape S, const uint64_t *__restrict__ turns)
 {
     __shared__ float2 trig[kTrig];
-    const int64_t token0 = (int64_t)blockIdx.x * S.tokens;
+    const int64_t token0 = (int64_t)(S.block0 + blockIdx.x) * S.tokens;
     const int n = (int)min((int64_t)S.tokens, A.n_tokens - token0);
     for (int e = threadIdx.x; e < n * S.pairs; e += kThreads) {
         const int t = e / S.pairs, p = e - t * S.pairs;
@@ -124,6 +125,7 @@ struct RowShape {
     int32_t heads;           // of q, k and (with a cache) v
     int32_t tokens;          // most of a workgroup
     int32_t head_dim, pairs;
+    uint32_t block0;         // first workgroup of the launch
     int64_t rows;            // of the call
 };
 
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowS
     __shared__ alignas(16) float cosine[kMostAngles], sine[kMostAngles];
     __shared__ int64_t place_in_cache[kMostTokens];
 
-    const int64_t row0 = (int64_t)blockIdx.x * (S.step * kRows);
+    const int64_t row0 = (int64_t)(S.block0 + blockIdx.x) * (S.step * kRows);
     const int64_t token0 = S.rows <= 0xFFFFFFFF ? (int64_t)((uint32_t)row0 / (uint32_t)S.heads) : row0 / S.heads;
     const int head0 = (int)(row0 - token0 * S.heads);
     const int lane_row = (int)threadIdx.x / S.units, u = (int)threadIdx.x - lane_row * S.units;
@@ -316,13 +318,16 @@ int launch_rows(const prep_rotary &R, const prep_rotary_args &A, hipStream_t str
     // Past the caches where what a load takes of a row is whole 128-byte lines: then 34 -> 30 us and 64 -> 58 us (the first and the last
     // of the calls above), 35 -> 29 for rows of 256 in bf16; pieces of 64 bytes 34 -> 34, of 80 and 96 bytes 44 -> 55 and 35 -> 39.
     const bool lines = S.units * 16 % 128 == 0 && rows_aligned(R, A, 128);
-    const dim3 grid((uint32_t)blocks);
-    if (per_lane == 1)
-        hipLaunchKernelGGL((rotary_rows<T, kHalves, 1, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
-    else if (!lines)
-        hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
-    else
-        hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    in_launches((uint32_t)blocks, kThreads, [&](uint32_t first, uint32_t n) {
+        const dim3 grid(n);
+        S.block0 = first;
+        if (per_lane == 1)
+            hipLaunchKernelGGL((rotary_rows<T, kHalves, 1, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+        else if (!lines)
+            hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+        else
+            hipLaunchKernelGGL((rotary_rows<T, kHalves, kManyRows, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    });
     return PREP_OK;
 }
 
@@ -337,11 +342,14 @@ int launch_for(const prep_rotary &R, const prep_rotary_args &A, hipStream_t stre
     S.tokens = kTrig / R.pairs < kMaxTokens ? kTrig / R.pairs : kMaxTokens;
     const int64_t blocks = (A.n_tokens + S.tokens - 1) / S.tokens;
     if (blocks > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
-    const dim3 grid((uint32_t)blocks);
-    if (halves)
-        hipLaunchKernelGGL((rotary_pairs<T, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
-    else
-        hipLaunchKernelGGL((rotary_pairs<T, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    in_launches((uint32_t)blocks, kThreads, [&](uint32_t first, uint32_t n) {
+        const dim3 grid(n);
+        S.block0 = first;
+        if (halves)
+            hipLaunchKernelGGL((rotary_pairs<T, true>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+        else
+            hipLaunchKernelGGL((rotary_pairs<T, false>), grid, dim3(kThreads), 0, stream, A, S, (const uint64_t *)R.d_turns);
+    });
     return PREP_OK;
 }
 

@@ -23,6 +23,18 @@ inline int element_bytes(int dtype) { return dtype == PREP_F32 ? 4 : 2; }
 inline bool float_type(int dtype) { return dtype == PREP_F32 || dtype == PREP_F16 || dtype == PREP_BF16; }
 inline bool aligned(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
+// Launches `blocks` workgroups of `threads`: launch(first, n) for n of them from `first` on, in as many launches as it takes, since HIP takes
+// fewer than 2^32 work-items along an axis.
+template <typename Launch>
+void in_launches(uint32_t blocks, int threads, const Launch &launch)
+{
+    const uint32_t most = 0xFFFFFFFFu / (uint32_t)threads;
+    for (uint32_t first = 0, n; first < blocks; first += n) {
+        n = blocks - first < most ? blocks - first : most;
+        launch(first, n);
+    }
+}
+
 // Makes `device` current and the caller's device current again at the end.
 class DeviceScope {
 public:

@@ -39,6 +39,11 @@ def _build(where, source, rest=""):
 
 
 @pytest.fixture(scope="module")
+def rotary(tmp_path_factory):
+    return _build(tmp_path_factory.mktemp("rotary"), "rotary.hip")
+
+
+@pytest.fixture(scope="module")
 def patches(tmp_path_factory):
     return _build(tmp_path_factory.mktemp("patches"), "patches.hip", "int prep::decode_batch(prep_handle *, const uint8_t *, const uint8_t *, const "
                   "uint64_t *, int32_t, OutputStage *, hipStream_t) { return PREP_E_INVALID_ARG; }")
@@ -84,7 +89,7 @@ def test_frames_of_more_than_2_31_pixels(patches, side, merge):
     patches.want(looked_at)
     rc, starts = _patch_rows(patches, params, picture.ctypes.data, w, w, 3 * w, out.ptr + below, rows)
     assert rc == 0 and starts == [0, rows]
-    weights = _enlarging_weights(w, side)
+    weights = enlarging_weights(w, side)
     for row in looked_at:
         y, x = place_of_row(row, cols, merge)
         wy, wx = weights(range(y * patch, (y + 1) * patch)), weights(range(x * patch, (x + 1) * patch))
@@ -95,7 +100,7 @@ def test_frames_of_more_than_2_31_pixels(patches, side, merge):
         cases.within(got, want, cases.patch_tolerance(w, w, side, side, True), "bf16")
 
 
-def _enlarging_weights(size, out):
+def enlarging_weights(size, out):
     def rows(which):
         m = np.zeros((len(which), size))
         for k, i in enumerate(which):
@@ -124,3 +129,99 @@ def test_rows_far_apart(patches, pitch, h):
     rc, starts = _patch_rows(patches, params, src.ptr, w, h, pitch, out.ctypes.data, len(want))
     assert rc == 0 and starts == [0, len(want)] and patches.launches()[-1][0] + patches.launches()[-1][1] <= 64
     cases.within(out.astype(np.float64), want, cases.patch_tolerance(w, h, ow, oh, True), "f32")
+
+
+MOST = 2 ** 32 - 1  # work-items of a launch along an axis, by HIP's documentation
+
+
+def in_launches_that_fit(launches):
+    """Launches follow one another without gaps and each has a size that HIP takes."""
+    at = 0
+    for before, groups, threads in launches:
+        assert before == at and 0 < groups and groups * threads <= MOST, launches
+        at += groups
+    return at
+
+
+@pytest.mark.parametrize("frames,group", [(1, 2), (3, 1)])
+def test_more_pixels_than_a_launch_has_work_items(patches, frames, group):
+    """65 520 x 65 520 pixels in two slots or three frames: rows at the seams of the launches, and the last."""
+    w, patch, side = 16, 16, 65520
+    params = prep.make_patch_params(patch, 1, group, "bf16", cases.MEAN, cases.STD, prep.FILTER_BILINEAR, min_pixels=side * side)
+    cols = side // patch
+    rows, area = cols * cols, patch * patch
+    picture = cases.picture(np.random.default_rng(6), (frames, w, w, 3))
+    out = Sparse(3 * area * 2 * group * rows * (-(-frames // group)))
+    total = rows * frames * group
+    looked_at = [0, rows, MOST // 256 - 1, MOST // 256, 2 * (MOST // 256), total - 1]  # (a workgroup has the 256 pixels of a patch)
+    looked_at = [r for r in looked_at if r < total]
+    patches.want(looked_at)
+    starts = (C.c_int64 * 2)()
+    rc = patches.lib.prep_patch_rows(0, C.c_void_p(picture.ctypes.data), prep._packed("Q", [0]), prep._packed("i", [w]), prep._packed("i", [w]),
+                                     prep._packed("i", [3 * w]), prep._packed("i", [frames]), prep._packed("Q", [3 * w * w]), 1, C.byref(params),
+                                     C.c_void_p(out.ptr), C.c_int64(0), C.c_int64(2 ** 40), starts, None)
+    assert rc == 0 and list(starts) == [0, rows * -(-frames // group)]
+    assert in_launches_that_fit(patches.launches()) == total
+    weights = enlarging_weights(w, side)
+    values = out.bytes.view(np.uint16).reshape(-1, 3, group, area)
+    for r in looked_at:
+        slot, row = divmod(r, rows)
+        y, x = divmod(row, cols)
+        wy, wx = weights(range(y * patch, (y + 1) * patch)), weights(range(x * patch, (x + 1) * patch))
+        v = np.stack([wy @ picture[min(slot, frames - 1), ..., c].astype(np.float64) @ wx.T for c in range(3)])
+        want = ((v / 255 - np.array(cases.MEAN)[:, None, None]) / np.array(cases.STD)[:, None, None]).reshape(3, area)
+        cases.within(cases.unpack(values[slot // group * rows + row, :, slot % group], "bf16"), want, cases.patch_tolerance(w, w, side, side, False), "bf16")
+
+
+def test_clips_of_more_tiles_than_a_launch_has_work_items(patches):
+    """Frames in tiles, 512 threads each: launches whose sizes HIP takes, one after another."""
+    params = prep.make_patch_params(16, 1, 1, "f16", cases.MEAN, cases.STD, prep.FILTER_ANTIALIAS, max_pixels=8000 * 2500)
+    w, h, frames = 20000, 6000, 4000
+    rows = np.prod(prep.patch_grid(params, w, h, frames))
+    starts = (C.c_int64 * 2)()
+    patches.want()
+    rc = patches.lib.prep_patch_rows(0, C.c_void_p(4096), prep._packed("Q", [0]), prep._packed("i", [w]), prep._packed("i", [h]), prep._packed("i", [3 * w]),
+                                     prep._packed("i", [frames]), prep._packed("Q", [3 * w * h]), 1, C.byref(params), C.c_void_p(4096), C.c_int64(0),
+                                     C.c_int64(2 ** 50), starts, None)
+    assert rc == 0 and list(starts) == [0, rows]
+    assert in_launches_that_fit(patches.launches()) * 512 > MOST
+
+
+def _rotary(library, head_dim, pairs, dtype):
+    h = C.c_void_p()
+    cfg = prep.RotaryConfig(0, head_dim, (C.c_int32 * 3)(pairs, 0, 0), {"f32": prep.F32, "bf16": prep.BF16}[dtype], 0, 0, 0, 0, 1e4, None)
+    assert library.lib.prep_rotary_create(C.byref(h), C.byref(cfg)) == 0
+    return h
+
+
+@pytest.mark.parametrize("head_dim,pairs,dtype", [(2, 1, "bf16"), (32, 16, "f32")])
+def test_more_rows_than_a_launch_has_work_items(rotary, head_dim, pairs, dtype):
+    """One head of many tokens, a thread a pair and rows in 16 bytes: tokens at the seams of the launches, and the last."""
+    n = 2 ** 31 - 1
+    size = 2 if dtype == "bf16" else 4
+    q, out, positions = Sparse(n * head_dim * size), Sparse(n * head_dim * size), Sparse(n * 4)
+    handle = _rotary(rotary, head_dim, pairs, dtype)
+
+    def call():
+        return rotary.lib.prep_rotary_apply(handle, prep._ROTARY_ARGS.pack(
+            n, positions.ptr, 0, q.ptr, head_dim, head_dim, out.ptr, head_dim, head_dim, *[0] * 9, 1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), None)
+
+    rotary.want()
+    assert call() == 0
+    launches = rotary.launches()
+    groups = in_launches_that_fit(launches)
+    assert len(launches) > 1
+    step = next(s for s in range(1, 1025) if -(-n // s) == groups)  # tokens of a workgroup
+    seams = [before for before, _, _ in launches] + [groups - 1]
+    tokens = sorted({t for s in seams for t in (s * step - 1, s * step, min(s * step + step, n) - 1) if 0 <= t < n})
+    rng = np.random.default_rng(3)
+    x = cases.unpack(cases.pack(rng.standard_normal((len(tokens), 1, head_dim)), dtype), dtype)
+    places = rng.integers(0, 2 ** 31, len(tokens))
+    given, taken = (b.bytes.view(cases.NUMPY[dtype]).reshape(n, head_dim) for b in (q, out))
+    given[tokens] = cases.pack(x[:, 0], dtype)
+    positions.bytes.view(np.int32)[tokens] = places
+    rotary.want([t // step for t in tokens])
+    assert call() == 0
+    rotary.lib.prep_rotary_destroy(handle)
+    want = oracle.rotary(x, np.stack([places] * 3), [0] * pairs, oracle.frequencies((pairs, 0, 0), 1e4, False, False), False, False)
+    cases.within(cases.unpack(taken[tokens], dtype), want[:, 0], cases.rotary_tolerance(x, pairs, False)[:, 0], dtype)
