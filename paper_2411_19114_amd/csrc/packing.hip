@@ -103,7 +103,8 @@ struct SegmentList {
 };
 __device__ __forceinline__ int32_t seq_bound(const SegmentList &L, int i) { return min(max(L.seq_segments[i], 0), L.n_segments); }
 
-// Tokens of a segment, and how far places move on; both 0 for one that is not valid.
+// Tokens of a segment (2^31 stand for more, so that sums over 2^20 segments stay in 64 bits: what lies behind that many tokens is beyond any
+// capacity), and how far places move on; both 0 for one that is not valid.
 __device__ __forceinline__ Sums segment_size(const prep_segment &s)
 {
     constexpr int32_t kMost = 32767;
@@ -112,7 +113,7 @@ __device__ __forceinline__ Sums segment_size(const prep_segment &s)
         return {n, n};
     }
     if (s.t < 1 || s.h < 1 || s.w < 1 || s.step < 0 || s.t > kMost || s.h > kMost || s.w > kMost || s.step > kMost) return {0, 0};
-    return {(uint64_t)s.t * (uint32_t)(s.h * s.w), (uint64_t)(uint32_t)(max(max((s.t - 1) * s.step, s.h - 1), s.w - 1) + 1)};
+    return {min((uint64_t)s.t * (uint32_t)(s.h * s.w), (uint64_t)1 << 31), (uint64_t)(uint32_t)(max(max((s.t - 1) * s.step, s.h - 1), s.w - 1) + 1)};
 }
 
 // Place of token r of a segment that starts at place `base`; h = 0: text.

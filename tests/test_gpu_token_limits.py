@@ -4,6 +4,7 @@ import pytest
 
 import paper_2411_19114_amd as prep
 import token_cases as cases
+from test_gpu_tokens import Backend
 from test_token_limits import MOST, enlarging_weights, place_of_row
 
 pytestmark = pytest.mark.gpu
@@ -60,3 +61,7 @@ def test_more_tokens_than_a_launch_has_work_items():
         for got, want in zip(out[at:at + step].double()[:n - at].unbind(1), (a * c - b * s, a * s + b * c)):
             limit = (a.abs() + b.abs()) * (cases.TRIG + 2 * cases.ULP) * (1 + cases.HALF_STEP["bf16"]) + want.abs() * cases.HALF_STEP["bf16"] + cases.LEAST_STEP["bf16"]
             assert ((got - want).abs() <= limit).all(), at
+
+
+def test_more_tokens_than_64_bits_count():
+    cases.check_more_tokens_than_64_bits_count(Backend())

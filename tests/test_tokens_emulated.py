@@ -67,3 +67,7 @@ def test_rotary_gradient():
 
 def test_refusals():
     run("check_patch_refusals", "check_packing_refusals", "check_rotary_refusals")
+
+
+def test_more_tokens_than_64_bits_count():
+    run("check_more_tokens_than_64_bits_count")

@@ -577,3 +577,26 @@ def check_bad_blocks(backend):
     """Blocks outside the cache, in the table and on the stack, give no slots."""
     check_slots(backend, "prompts", bad_ids=True)
     check_slots(backend, "step", bad_ids=True)
+
+
+def check_more_tokens_than_64_bits_count(backend):
+    """Segments of 2^64 tokens together: the sum does not wrap, and the first places are right."""
+    most, left = 32767, 2 ** 64
+    segments = [(2, 0, 0, 0)] + [(most, most, most, 1)] * ((left - 2) // most ** 3)
+    left -= sum(t * h * w for t, h, w, _ in segments[1:]) + 2
+    for t, h in ((most, most), (1, most)):
+        segments.append((t, h, left // (t * h), 1))
+        left -= t * h * segments[-1][2]
+    segments.append((left, 0, 0, 0))
+    assert len(segments) <= 1 << 20 and left > 0
+    n, capacity = len(segments), 5000
+    flat, seq = backend.put(np.array(segments, dtype=np.int32)), backend.put(np.array([0, n - 1, n], dtype=np.int32))
+    positions, starts = backend.put(np.full((3, capacity), 77, dtype=np.int32)), backend.put(np.full(3, 77, dtype=np.int32))
+    size = prep.token_positions_workspace(n)
+    work = backend.put(np.zeros(size, dtype=np.uint8))
+    prep.token_positions(backend.ptr(flat), n, backend.ptr(seq), 2, 0, 1, backend.ptr(positions), capacity, backend.ptr(starts), 0, backend.ptr(work), size,
+                         stream=backend.stream)
+    assert backend.get(starts).tolist() == [0, 2 ** 31 - 1, 2 ** 31 - 1]
+    i = np.arange(capacity - 2)
+    want = np.stack([np.append([0, 1], 2 + v) for v in (0 * i, i // most, i % most)])
+    assert np.array_equal(backend.get(positions), want)
