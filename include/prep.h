@@ -573,8 +573,9 @@ int prep_block_slots(int32_t device, const prep_block_args *args, void *stream);
  *             i < 3 sections[2] axis 2; the others axis 0 (the sections must come out)
  *   f       : frequencies[i] (HOST, n entries, radians a place) if given; else base^(-i / n); with
  *             PREP_ROTARY_PER_AXIS base^(-j / sections[axis]) for the axis' j-th pair
- * The angle is taken in 64-bit fixed point, modulo a turn, so it is as exact at place 2^30 as at
- * place 1; sums are fp32, rounded once to the element type. */
+ * f / 2 pi is held to 2^-62 of a turn (above one turn a place: to 2^-62 of itself), and the angle is its 64-bit product with the place, modulo a
+ * turn: up to f = 2 pi off by at most 2^-31 of a turn at place 2^31 - 1, by less at nearer ones.  Its cos and sin are fp32, off by at most 3e-7,
+ * the sine of up to an eighth of a turn by at most 5e-7 of itself; products and sums are fp32, rounded once to the element type. */
 enum { PREP_PAIR_HALVES = 0, PREP_PAIR_ADJACENT = 1 };
 enum { PREP_SECTIONS_BLOCKS = 0, PREP_SECTIONS_INTERLEAVED = 1 };
 enum { PREP_ROTARY_PER_AXIS = 1 };

@@ -15,8 +15,8 @@
 
 struct prep_rotary {
     int32_t device, head_dim, pairs, dtype, pairing;
-    uint64_t *d_turns;  // per pair: turns a place, as a fraction of 2^64; the two lowest bits hold the axis (2^-62 of a
-                        // turn, 2^-31 at the farthest place, below an fp32 angle's last bit)
+    uint64_t *d_turns;  // per pair: turns a place, as a fraction of 2^64, to the nearest multiple of four: the two lowest bits hold
+                        // the axis (so it is off by 2^-63 of a turn at most, and 2^-32 at the farthest place)
 };
 
 namespace prep {
@@ -34,12 +34,13 @@ struct RotaryShape {
 };
 
 // cos and sin of a fraction of a turn.  Reduced to an eighth of a turn either side of a quadrant's middle
-// axis; there Taylor's series up to x^9 and x^10 leave 2e-9 and 1.2e-10.
+// axis; there Taylor's series up to x^9 and x^10 leave 2e-9 and 1.2e-10.  The angle is the sum of its upper 32 bits, rounded, and of the
+// rest, with its sign, so that a small one (a slow pair's at a near place) has all the bits of a float.
 __device__ __forceinline__ float2 cos_sin(uint64_t phase)
 {
     const uint32_t turn = (uint32_t)((phase + 0x80000000ull) >> 32);
     const uint32_t quadrant = (turn + 0x20000000u) >> 30;
-    const float x = (float)(int32_t)(turn - (quadrant << 30)) * 1.4629180792671596e-9f;  // 2 pi / 2^32
+    const float x = fmaf((float)(int32_t)(turn - (quadrant << 30)), 4294967296.0f, (float)(int32_t)(uint32_t)phase) * 3.4061215800865545e-19f;  // 2 pi / 2^64
     const float z = x * x;
     const float s = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), 1.0f);
     const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);

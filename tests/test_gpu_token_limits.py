@@ -65,3 +65,8 @@ def test_more_tokens_than_a_launch_has_work_items():
 
 def test_more_tokens_than_64_bits_count():
     cases.check_more_tokens_than_64_bits_count(Backend())
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_slow_pairs(adjacent):
+    cases.check_slow_pairs(Backend(), adjacent)

@@ -71,3 +71,7 @@ def test_refusals():
 
 def test_more_tokens_than_64_bits_count():
     run("check_more_tokens_than_64_bits_count")
+
+
+def test_slow_pairs():
+    run("check_slow_pairs:False", "check_slow_pairs:True")

@@ -600,3 +600,27 @@ def check_more_tokens_than_64_bits_count(backend):
     i = np.arange(capacity - 2)
     want = np.stack([np.append([0, 1], 2 + v) for v in (0 * i, i // most, i % most)])
     assert np.array_equal(backend.get(positions), want)
+
+
+def check_slow_pairs(backend, adjacent=False):
+    """sin of small angles (a = 1, b = 0), against the formula in extended precision, relative to itself: the angle is rounded when its parts
+    become floats, when these are added, with the constant 2 pi and with the product, the series' terms and the result once each: 8 half steps
+    of 2^-24; a frequency is held to 2^-63 of a turn, 2^-22 of one being the slowest here, and x^11 / 11! left out, 3e-9 of sin x."""
+    d, base, places = 128, 1e6, np.array([1, -1, 2, 7, -50, 1000, 30000, -777777], dtype=np.int64)
+    n, pairs = len(places), d // 2
+    x = np.zeros((n, 1, d), dtype=np.float32)
+    x[..., 0:d:2] = 1.0 if adjacent else 0.0
+    if not adjacent:
+        x[..., :pairs] = 1.0
+    given, out = backend.put(x), backend.put(np.zeros_like(x))
+    positions = backend.put(places.astype(np.int32))
+    rotary = prep.Rotary(d, (pairs, 0, 0), base, "f32", pairing=int(adjacent))
+    rotary.apply(n, backend.ptr(positions), n, q=(backend.ptr(given), d, d), q_out=(backend.ptr(out), d, d), q_heads=1, stream=backend.stream)
+    got = backend.get(out)[:, 0].astype(np.longdouble)
+    rotary.close()
+    sine = got[:, 1::2] if adjacent else got[:, pairs:]
+    angle = places[:, None].astype(np.longdouble) * np.array(oracle.frequencies((pairs, 0, 0), base, False, False))[None]
+    small = np.abs(angle) <= np.pi / 4
+    assert small.sum() > 200 and np.abs(angle).min() < 2e-6
+    want = np.sin(angle)
+    assert (np.abs(sine - want)[small] <= np.abs(want)[small] * (8 * ULP + 3e-9 + 2.0 ** -40)).all()
