@@ -521,6 +521,8 @@ def patch_rows(device, rgb_ptr, rgb_offsets, widths, heights, pitches, params, o
                out_stride=0, stream=0):
     """prep_patch_rows: patch rows of decoded frames; returns where each clip's rows begin, and their number."""
     n = len(widths)
+    if any(x is not None and len(x) != n for x in (rgb_offsets, heights, pitches, frames, frame_strides)):
+        raise PrepError(E_INVALID_ARG, "prep_patch_rows")
     starts = (C.c_int64 * (n + 1))()
     _check(lib().prep_patch_rows(
         device, rgb_ptr, _packed("Q", rgb_offsets), _packed("i", widths), _packed("i", heights), _packed("i", pitches),

@@ -225,3 +225,16 @@ def test_more_rows_than_a_launch_has_work_items(rotary, head_dim, pairs, dtype):
     rotary.lib.prep_rotary_destroy(handle)
     want = oracle.rotary(x, np.stack([places] * 3), [0] * pairs, oracle.frequencies((pairs, 0, 0), 1e4, False, False), False, False)
     cases.within(cases.unpack(taken[tokens], dtype), want[:, 0], cases.rotary_tolerance(x, pairs, False)[:, 0], dtype)
+
+
+@pytest.mark.parametrize("short", ["rgb_offsets", "heights", "pitches", "frames", "frame_strides"])
+def test_lists_of_different_lengths(short, monkeypatch):
+    """The binding refuses them: the call would read behind the shorter one."""
+    def never(*_):
+        raise AssertionError("called")
+
+    monkeypatch.setattr(prep, "_lib", type("Library", (), {"prep_patch_rows": never, "prep_strerror": lambda *_: b""})())
+    lists = {"rgb_offsets": [0, 768], "widths": [16, 16], "heights": [16, 16], "pitches": [48, 48], "frames": [1, 1], "frame_strides": [768, 768]}
+    lists[short] = lists[short][:1]
+    params = prep.make_patch_params(16, 1, 1, "f32", cases.MEAN, cases.STD)
+    cases.refused(prep.E_INVALID_ARG, prep.patch_rows, 0, 4096, params=params, out_ptr=8192, out_rows=2, **lists)
