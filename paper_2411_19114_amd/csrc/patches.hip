@@ -804,14 +804,14 @@ public:
         c.across = c.down = c.part_rows = c.parts = 1;  // (direct)
         c.frames = frames;
         c.image = i;
-        row_starts_[i + 1] = row_starts_[i] + groups * rows * cols;
+        if (__builtin_add_overflow(row_starts_[i], groups * rows * cols, &row_starts_[i + 1])) row_starts_[i + 1] = INT64_MAX;
         next_ = i + 1;
         return true;
     }
     int finish()
     {
         skip_to(n_);
-        return row_starts_[n_] > out_rows_ ? PREP_E_TOO_LARGE : PREP_OK;
+        return row_starts_[n_] > out_rows_ || row_starts_[n_] == INT64_MAX ? PREP_E_TOO_LARGE : PREP_OK;
     }
     int launch(const uint8_t *rgb, const int32_t *status, hipStream_t stream)
     {

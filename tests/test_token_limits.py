@@ -238,3 +238,18 @@ def test_lists_of_different_lengths(short, monkeypatch):
     lists[short] = lists[short][:1]
     params = prep.make_patch_params(16, 1, 1, "f32", cases.MEAN, cases.STD)
     cases.refused(prep.E_INVALID_ARG, prep.patch_rows, 0, 4096, params=params, out_ptr=8192, out_rows=2, **lists)
+
+
+def test_more_rows_than_64_bits_count(patches):
+    """2^24 + 9 clips of nearly 2^39 rows each are too many for any output, and nothing is enqueued."""
+    n, frames = 2 ** 24 + 9, 2 ** 31 - 1
+    params = prep.make_patch_params(1, 1, 1, "bf16", cases.MEAN, cases.STD)
+    side, stride = np.full(n, 16, dtype=np.int32), np.full(n, 48 * 16, dtype=np.uint64)
+    arrays = [np.zeros(n, dtype=np.uint64), side, side, np.full(n, 48, dtype=np.int32), np.full(n, frames, dtype=np.int32), stride]
+    starts = np.zeros(n + 1, dtype=np.int64)
+    assert n * frames * 256 > 2 ** 63
+    patches.want()
+    rc = patches.lib.prep_patch_rows(0, C.c_void_p(4096), *[C.c_void_p(a.ctypes.data) for a in arrays], n, C.byref(params), C.c_void_p(4096), C.c_int64(0),
+                                     C.c_int64(2 ** 50), C.c_void_p(starts.ctypes.data), None)
+    assert rc == prep.E_TOO_LARGE and patches.launches() == []
+    assert (np.diff(starts) >= 0).all() and starts[-1] == 2 ** 63 - 1
