@@ -1,4 +1,4 @@
-"""Calls of the operators for packed batches of tokens whose sizes pass 32 bits, on the GPU."""
+"""The operators for packed batches of tokens on the GPU: calls whose sizes pass 32 bits, and what test_gpu_tokens.py leaves out."""
 import numpy as np
 import pytest
 
@@ -70,3 +70,19 @@ def test_more_tokens_than_64_bits_count():
 @pytest.mark.parametrize("adjacent", [False, True])
 def test_slow_pairs(adjacent):
     cases.check_slow_pairs(Backend(), adjacent)
+
+
+@pytest.mark.parametrize("name", cases.PATCHES_MORE)
+def test_clips_over_several_launches(name):
+    cases.check_more_patches(Backend(), name)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_given_frequencies(adjacent, dtype):
+    cases.check_given_frequencies(Backend(), adjacent, dtype)
+
+
+@pytest.mark.parametrize("many", [False, True])
+def test_segments_of_no_sequence(many):
+    cases.check_segments_of_no_sequence(Backend(), many)

@@ -75,3 +75,16 @@ def test_more_tokens_than_64_bits_count():
 
 def test_slow_pairs():
     run("check_slow_pairs:False", "check_slow_pairs:True")
+
+
+@pytest.mark.parametrize("name", cases.PATCHES_MORE)
+def test_clips_over_several_launches(name):
+    run(f"check_more_patches:{name}")
+
+
+def test_given_frequencies():
+    run("check_given_frequencies:False", "check_given_frequencies:True")
+
+
+def test_segments_of_no_sequence():
+    run("check_segments_of_no_sequence:False", "check_segments_of_no_sequence:True")

@@ -624,3 +624,66 @@ def check_slow_pairs(backend, adjacent=False):
     assert small.sum() > 200 and np.abs(angle).min() < 2e-6
     want = np.sin(angle)
     assert (np.abs(sine - want)[small] <= np.abs(want)[small] * (8 * ULP + 3e-9 + 2.0 ** -40)).all()
+
+
+# ---- clips over several launches, given frequencies, segments of no sequence ------------------------------------------------
+
+# (a launch takes 64 clips of a kind; those narrower than 6 pixels are of a kind of their own)
+PATCHES_MORE = {
+    "several_launches": ([(4 + i % 5, 4 + i % 3) for i in range(330)], [1] * 330, 4, 1, 1, "f16", True, 0, 0),
+    "several_launches_of_clips": ([(3 + i % 7, 9 - i % 4) for i in range(150)], [1 + i % 3 for i in range(150)], 3, 1, 2, "f32", False, 0, 0),
+}
+
+def check_more_patches(backend, name):
+    PATCHES_LARGE[name] = PATCHES_MORE[name]
+    try:
+        check_patches(backend, name)
+    finally:
+        del PATCHES_LARGE[name]
+
+
+# frequencies in radians a place: negative, zero, whole turns, above a turn
+FREQUENCIES = [0.0, -0.0, 1.0, -1.0, 0.3, -0.7, 1e-6, -1e-9, 2 * math.pi, -2 * math.pi, math.pi, 5.5, -6.2, 1e-3, -0.05, 2.0 ** -20]
+
+
+def check_given_frequencies(backend, adjacent, dtype="f32"):
+    """The base is not looked at, and a negative frequency turns the other way."""
+    n, h, d, pairs = 12, 2, 40, len(FREQUENCIES)
+    rng = np.random.default_rng(7)
+    x = unpack(pack(rng.standard_normal((n, h, d)), dtype), dtype)
+    positions = rng.integers(-2000, 2000, (3, n))
+    positions[:, :2] = [[2 ** 30, -2 ** 31]] * 3
+    sections = (5, 6, 5)
+    given, out = backend.put(pack(x, dtype)), backend.put(pack(np.zeros_like(x), dtype))
+    places = backend.put(positions.astype(np.int32))
+    rotary = prep.Rotary(d, sections, float("nan"), dtype, pairing=int(adjacent), per_axis=True, frequencies=FREQUENCIES)
+    rotary.apply(n, backend.ptr(places), n, q=(backend.ptr(given), h * d, d), q_out=(backend.ptr(out), h * d, d), q_heads=h, stream=backend.stream)
+    got = unpack(backend.get(out), dtype)
+    rotary.close()
+    # the oracle's angle is a product of 64 bits, whose half step at 2^31 places of 2 pi is 2^-31 radians; the call's is off by 2^-31 of a turn
+    extra = 2.0 ** -31 * (1 + 2 * math.pi)
+    want = oracle.rotary(x, positions, oracle.pair_axes(sections, False), FREQUENCIES, adjacent, False)
+    within(got, want, rotary_tolerance(x, pairs, adjacent) * (1 + extra / TRIG), dtype)
+    assert np.array_equal(got[..., 2 * pairs:], x[..., 2 * pairs:])
+
+
+def check_segments_of_no_sequence(backend, many):
+    """Segments before the first sequence's and behind the last one's count for nothing, and bounds outside the list are its ends."""
+    piece = [T(2), G(1, 2, 3), T(0), G(2, 3, 1, 4), T(1)]
+    flat = piece * (1000 if many else 6)
+    n = len(flat)
+    for bounds in ([3, 3, 9, n - 4], [-7, 2, 5, n - 1], [1, n - 2, n, n + 50], [-3, -1, n + 1, n + 9], [n, n, n, n], [-9, -9, -9, -9]):
+        clamped = np.clip(bounds, 0, n)
+        first = [10, -3, 500]
+        want, starts, nexts = oracle.token_positions([flat[a:b] for a, b in zip(clamped, clamped[1:])], first, 2)
+        capacity = starts[-1] + 6
+        segments, seq, base = backend.put(np.array(flat, dtype=np.int32)), backend.put(np.array(bounds, dtype=np.int32)), backend.put(np.array(first, dtype=np.int32))
+        positions, token_starts, nxt = (backend.put(np.full(m, 77, dtype=np.int32)) for m in (3 * capacity, 4, 3))
+        size = prep.token_positions_workspace(n)
+        work = backend.put(np.full(size, 77, dtype=np.uint8))
+        prep.token_positions(backend.ptr(segments), n, backend.ptr(seq), 3, backend.ptr(base), 2, backend.ptr(positions), capacity, backend.ptr(token_starts),
+                             backend.ptr(nxt), backend.ptr(work), size, stream=backend.stream)
+        full = np.zeros((3, capacity), dtype=np.int64)
+        full[:, :starts[-1]] = want
+        assert np.array_equal(backend.get(positions).reshape(3, capacity), full), bounds
+        assert backend.get(token_starts).tolist() == starts and backend.get(nxt).tolist() == nexts, bounds
