@@ -49,7 +49,8 @@ __host__ __device__ __forceinline__ Divisor divisor(int d) { return {(uint32_t)d
 constexpr int kTileCols = 64, kTileRows = 16, kPatches = 128;
 constexpr int kStrip = 4;                          // tiles one below the other that a workgroup takes, at most (2: 205 us for 196, 84 for 75)
 constexpr int kNarrowest = 6;                      // narrowest image whose rows hold a read of 16 bytes
-constexpr int kFewTaps = 3, kSomeTaps = 5;          // columns of a window whose weights stay in registers
+constexpr int kFewTaps = 3, kMostTaps = 6;          // columns of a window whose weights stay in registers
+constexpr int kSomeTaps = 5;                       // fewer than kMostTaps, where a window has no more
 constexpr float kWeightScale = 32768.0f;
 template <bool kWide, int kElement>
 struct Limits {
@@ -184,7 +185,7 @@ __device__ __forceinline__ void write_runs(const T *stage, const int32_t *row, i
     }
 }
 
-// A lane's output column: its window in the row's sums, kTaps samples wide, and their weights; kTaps = 0: any width, weights formed for
+// A lane's output column: its window in the row's sums, at most kTaps samples wide, and their weights; kTaps = 0: any width, weights formed for
 // every row.
 template <int kTaps>
 struct Column {
@@ -192,9 +193,10 @@ struct Column {
     int taps;    // kTaps = 0
     float centre, inv, norm;
     float w[kTaps != 0 ? kTaps : 1];
-    // a window starts earlier where kTaps samples would end behind the row's sums; what is not under the triangle has weight 0
-    __device__ __forceinline__ Column(int first, int taps_, float centre_, float inv_, float norm_, int most)
-        : at(kTaps != 0 ? min(first, most - kTaps) : first), taps(taps_), centre(centre_), inv(inv_), norm(norm_)
+    // `used` samples are summed, at most kTaps: a window starts earlier where they would end behind the row's sums; what is not under the
+    // triangle has weight 0
+    __device__ __forceinline__ Column(int first, int taps_, float centre_, float inv_, float norm_, int most, int used)
+        : at(kTaps != 0 ? min(first, most - used) : first), taps(taps_), centre(centre_), inv(inv_), norm(norm_)
     {
 #pragma unroll
         for (int k = 0; k < kTaps; k++) {
@@ -202,13 +204,14 @@ struct Column {
             w[k] = tap >= 0 && tap < taps ? fmaxf(0.0f, fmaf(-fabsf((float)tap - centre), inv, 1.0f)) * norm : 0.0f;
         }
     }
+    template <int kUsed>
     __device__ __forceinline__ void sum(const float *summed, float v[3]) const
     {
         const float *s = summed + at * 3;
         v[0] = v[1] = v[2] = 0.0f;
         if (kTaps != 0) {
 #pragma unroll
-            for (int k = 0; k < kTaps; k++)
+            for (int k = 0; k < kUsed; k++)
 #pragma unroll
                 for (int c = 0; c < 3; c++) v[c] = fmaf(w[k], s[3 * k + c], v[c]);
         } else {
@@ -220,13 +223,13 @@ struct Column {
         }
     }
 };
-template <typename T, int kTaps, int kSumPitch, int kWaves>
+template <typename T, int kUsed, int kTaps, int kSumPitch, int kWaves>
 __device__ __forceinline__ void sum_columns(const Column<kTaps> &column, const float *summed, T *stage, const int32_t *row_stage, int tile_h, int x_stage,
                                             int run, const PatchGeometry &g)
 {
     for (int t = uniform((int)threadIdx.x >> 6); t < tile_h; t += kWaves) {
         float v[3];
-        column.sum(summed + t * kSumPitch, v);
+        column.template sum<kUsed>(summed + t * kSumPitch, v);
         T *o = stage + uniform(row_stage[t]) + x_stage;
 #pragma unroll
         for (int c = 0; c < 3; c++) o[c * run] = from_float<T>(fmaf(v[c], g.scale[c], g.bias[c]));
@@ -330,10 +333,14 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
     }
 
     // the lane's output column
-    constexpr int kColumnTaps = kWide ? kSomeTaps : kFewTaps;
+    // (48 full-HD frames, bf16, us.  Windows of up to 5 samples, with 5 and with 6 summed: reduced 1.6 times 277 and 285, 2.3 times 180 and 181.
+    // Windows of 6, with weights kept and with weights formed for every row, as larger ones have them: 2.5 times 200 and 221, 2.7 times 180
+    // and 197, 2.9 times 222 and 248.)
+    constexpr int kColumnTaps = kWide ? kMostTaps : kFewTaps;
     const int x = min(lane, tile_w - 1), patch = (int)g.by_patch.quotient((uint32_t)x);
-    const bool any_taps = kWide && antialias && 2 * (int)C.width >= kSomeTaps * C.cols * g.patch;  // (columns_of_window > kSomeTaps)
-    const Column<kColumnTaps> column(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], groups * 64 / 3);
+    const bool any_taps = kWide && antialias && 2 * (int)C.width >= kMostTaps * C.cols * g.patch;  // (columns_of_window > kMostTaps)
+    const bool some_taps = kWide && !(antialias && 2 * (int)C.width >= kSomeTaps * C.cols * g.patch);
+    const Column<kColumnTaps> column(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], groups * 64 / 3, some_taps ? kSomeTaps : kColumnTaps);
 
     // what is written at a time, of a patch's channel in a tile, and in the last tile of a patch that several share
     Divisor whole_part = g.by_chunks, last_part = g.by_chunks;
@@ -442,11 +449,13 @@ __global__ __launch_bounds__((Limits<kWide, (int)sizeof(T)>::threads), (Limits<k
                 if (lane < tile_w) {
                     const int x_stage = patch * 3 * run + (x - patch * g.patch);
                     const int32_t *rows = row_stage + i * kTileRows;
-                    if (!any_taps) {
-                        sum_columns<T, kColumnTaps, kSumPitch, kWaves>(column, summed, stage, rows, tile_h, x_stage, run, g);
+                    if (some_taps) {
+                        sum_columns<T, kSomeTaps < kColumnTaps ? kSomeTaps : kColumnTaps, kColumnTaps, kSumPitch, kWaves>(column, summed, stage, rows, tile_h, x_stage, run, g);
+                    } else if (!any_taps) {
+                        sum_columns<T, kColumnTaps, kColumnTaps, kSumPitch, kWaves>(column, summed, stage, rows, tile_h, x_stage, run, g);
                     } else {
-                        const Column<0> wide(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], 0);
-                        sum_columns<T, 0, kSumPitch, kWaves>(wide, summed, stage, rows, tile_h, x_stage, run, g);
+                        const Column<0> wide(col_first[x] - c0, col_taps[x], col_centre[x], inv_x, col_norm[x], 0, 0);
+                        sum_columns<T, 0, 0, kSumPitch, kWaves>(wide, summed, stage, rows, tile_h, x_stage, run, g);
                     }
                 }
             } else {

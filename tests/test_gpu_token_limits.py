@@ -73,7 +73,7 @@ def test_slow_pairs(adjacent):
 
 
 @pytest.mark.parametrize("name", cases.PATCHES_MORE)
-def test_clips_over_several_launches(name):
+def test_more_patch_rows(name):
     cases.check_more_patches(Backend(), name)
 
 

@@ -78,7 +78,7 @@ def test_slow_pairs():
 
 
 @pytest.mark.parametrize("name", cases.PATCHES_MORE)
-def test_clips_over_several_launches(name):
+def test_more_patch_rows(name):
     run(f"check_more_patches:{name}")
 
 
