@@ -648,23 +648,40 @@ bool cut_into_tiles(PatchClip *c, const PatchGeometry &g, int64_t out_stride)
 // The kernels: patch_rows_direct, patch_rows_tiled with kWide = false and true.
 enum { kDirect = 0, kNarrow = 1, kWide = 2, kKinds = 3 };
 
-// Cuts the clips of a call into tiles.  One launch takes them all (two would wait for each other's last workgroups, 10 us or more), of the narrow kind where
-// every clip's tiles are as large as the wide kind's: it keeps four workgroups on a compute unit where the wide one keeps two.  Threads of a
-// workgroup, 256 and 512, us: narrow 28.5 and 41 (32 photographs), wide 266 and 196 (48 full-HD frames).
+// Cuts the clips of a call into tiles.  The narrow kind is for clips whose tiles are as large there as the wide kind's: it keeps four
+// workgroups on a compute unit where the wide one keeps two.  Clips of both kinds take a launch each if the narrow ones have 2^22 pixels or
+// more, some four rounds of the chip; with fewer the wait for one launch's last workgroups costs more, and one launch of the wide kind takes all.  us in one
+// launch and in two, antialiased, fp16: photographs of 400 x 365 with one picture of 4000 x 3000 reduced to 2^20 pixels, 4 of them 54 and 59, 16 of them 61 and
+// 62, 32 of them 76 and 72, 128 of them 180 and 132; frames of 380 x 285 up to 520 x 390 reduced to 147 456 pixels where they have more, 96 of them
+// 106 and 90, 256 of them 263 and 193; two taps, fp32, of 300 x 225 up to 900 x 675, 64 of them 77 and 84, 96 of them 125 and 114.
+// Threads of a workgroup, 256 and 512, us: narrow 28.5 and 41 (32 photographs), wide 266 and 196 (48 full-HD frames).
+constexpr uint64_t kOwnLaunchPixels = 1 << 22;
 template <int kElement>
 void cut_clips(PatchClip *clips, uint8_t *kinds, int32_t n, const PatchGeometry &g, int64_t out_stride)
 {
-    bool narrow = true;
+    const auto few_taps = [&](const PatchClip &c) { return columns_of_window(c.scale_x(g.patch), g.antialias) <= kFewTaps; };
+    const auto pixels = [&](const PatchClip &c) { return (uint64_t)c.frames * c.cols * c.rows * (uint64_t)(g.patch * g.patch); };
+    uint64_t few = 0, narrow = 0;
+    for (int32_t i = 0; i < n; i++)
+        if (few_taps(clips[i])) few += pixels(clips[i]);
+    const bool may_part = few >= kOwnLaunchPixels;
+    bool all = true;  // those looked at so far are of the narrow kind
     for (int32_t i = 0; i < n; i++) {
         PatchClip &c = clips[i], other = c;
         kinds[i] = cut_into_tiles<Limits<true, kElement>>(&c, g, out_stride) ? kWide : kDirect;
-        if (kinds[i] == kWide)
-            narrow = narrow && columns_of_window(c.scale_x(g.patch), g.antialias) <= kFewTaps && cut_into_tiles<Limits<false, kElement>>(&other, g, out_stride) &&
-                     other.across * other.down * other.part_rows >= c.across * c.down * c.part_rows;
+        if (kinds[i] == kDirect || (!may_part && !all)) continue;
+        if (few_taps(c) && cut_into_tiles<Limits<false, kElement>>(&other, g, out_stride) &&
+            other.across * other.down * other.part_rows >= c.across * c.down * c.part_rows) {
+            c = other;
+            kinds[i] = kNarrow;
+            narrow += pixels(c);
+        } else {
+            all = false;
+        }
     }
-    if (!narrow) return;
+    if (all || narrow >= kOwnLaunchPixels) return;
     for (int32_t i = 0; i < n; i++)
-        if (kinds[i] == kWide && cut_into_tiles<Limits<false, kElement>>(&clips[i], g, out_stride)) kinds[i] = kNarrow;
+        if (kinds[i] == kNarrow && cut_into_tiles<Limits<true, kElement>>(&clips[i], g, out_stride)) kinds[i] = kWide;
 }
 
 uint64_t groups_of(const PatchClip &c, const PatchGeometry &g) { return (uint64_t)((c.frames - 1) / g.group + 1); }

@@ -72,7 +72,7 @@ def test_slow_pairs(adjacent):
     cases.check_slow_pairs(Backend(), adjacent)
 
 
-@pytest.mark.parametrize("name", cases.PATCHES_MORE)
+@pytest.mark.parametrize("name", cases.PATCHES_MORE | cases.PATCHES_MIXED)
 def test_more_patch_rows(name):
     cases.check_more_patches(Backend(), name)
 

@@ -253,3 +253,16 @@ def test_more_rows_than_64_bits_count(patches):
                                      C.c_int64(2 ** 50), C.c_void_p(starts.ctypes.data), None)
     assert rc == prep.E_TOO_LARGE and patches.launches() == []
     assert (np.diff(starts) >= 0).all() and starts[-1] == 2 ** 63 - 1
+
+
+@pytest.mark.parametrize("photographs,large,threads", [(30, 0, [256]), (30, 1, [256, 512]), (4, 1, [512]), (0, 2, [512]), (200, 3, [256] * 4 + [512])])
+def test_large_pictures_among_photographs(patches, photographs, large, threads):
+    """Many photographs keep the kernel for tiles with small windows (256 threads) when a picture that is reduced comes with them."""
+    n = photographs + large
+    sizes = [(4000, 3000) if i < large else (480, 360) for i in range(n)]
+    params = prep.make_patch_params(16, 2, 1, "f16", cases.MEAN, cases.STD, prep.FILTER_ANTIALIAS, max_pixels=1 << 20)
+    starts = (C.c_int64 * (n + 1))()
+    patches.want()
+    rc = patches.lib.prep_patch_rows(0, C.c_void_p(4096), prep._packed("Q", [0] * n), prep._packed("i", [w for w, _ in sizes]), prep._packed("i", [h for _, h in sizes]),
+                                     prep._packed("i", [3 * w for w, _ in sizes]), None, None, n, C.byref(params), C.c_void_p(4096), C.c_int64(0), C.c_int64(2 ** 30), starts, None)
+    assert rc == 0 and [t for _, _, t in patches.launches()] == threads

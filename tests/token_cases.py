@@ -641,12 +641,15 @@ PATCHES_MORE = {
 }
 
 def check_more_patches(backend, name):
-    PATCHES_LARGE[name] = PATCHES_MORE[name]
+    PATCHES_LARGE[name] = (PATCHES_MORE | PATCHES_MIXED)[name]
     try:
         check_patches(backend, name)
     finally:
         del PATCHES_LARGE[name]
 
+
+# many photographs with larger pictures between them, in launches of two kinds (a GPU's)
+PATCHES_MIXED = {"large_mixed": ([(640, 480)] * 7 + [(1500, 1200)] + [(640, 480)] * 7, [1] * 15, 16, 2, 1, "f16", True, 0, 640 * 480)}
 
 # frequencies in radians a place: negative, zero, whole turns, above a turn
 FREQUENCIES = [0.0, -0.0, 1.0, -1.0, 0.3, -0.7, 1e-6, -1e-9, 2 * math.pi, -2 * math.pi, math.pi, 5.5, -6.2, 1e-3, -0.05, 2.0 ** -20]
