@@ -445,7 +445,8 @@ enum { PREP_BF16 = 3 };    /* a third element type, of these calls only         
  * [3][frames_per_patch][patch][patch]; the rows of a clip come frame group by frame group,
  * in a group window by window (merge x merge patches, windows in raster order, patches in
  * raster order inside), so that merge * merge rows in a row make one token of a model that
- * merges them.  The last frame stands in for frames that the last group lacks. */
+ * merges them.  The last frame stands in for frames that the last group lacks.  Weights along the height are held to 22 bits where
+ * samples go through the matrix cores (24 otherwise and along the width), whatever the element type; sums are fp32, rounded once to it. */
 typedef struct {
     int32_t patch;             /* 1..64                                             */
     int32_t merge;             /* 1..16                                             */
@@ -538,8 +539,9 @@ int prep_token_positions(int32_t device, const prep_segment *segments, int32_t n
  *   lengths        DEVICE, n entries: tokens of the request in the cache afterwards
  *   status         DEVICE, n entries: PREP_OK; PREP_E_INVALID_ARG (a negative length; the request then
  *                  has no tokens and length 0); PREP_E_TOO_LARGE: the request lacks blocks or its row of the
- *                  table or `slots` ends too early; it takes no block and its length stays (requests
- *                  behind one that the stack could not serve get no block either; those that need none are served)
+ *                  table or `slots` ends too early (for a request without new tokens: before the place
+ *                  where they would begin); it takes no block and its length stays (requests behind one that the
+ *                  stack could not serve get no block either; those that need none are served)
  *   free_left      DEVICE, one entry, another than free_count: blocks left on the stack.  A caller that keeps
  *                  the stack passes it as the next call's free_count.
  *   workspace      as above, prep_block_slots_workspace(n) bytes

@@ -220,9 +220,9 @@ __global__ __launch_bounds__(kThreads) void place_tokens(SegmentList L, const in
     }
 }
 
-// One launch, for at most kThreads * kEntries segments and sequences.  In a graph 4.5 us for 64 sequences of a token, 8.8 for 2000
-// segments of 400 000 tokens; bound by the chain of reads, sum and search, not by the 5 MB.  At 4096 segments 9 to 12 us by the number of
-// tokens; the two launches take 14 to 24 at 4097.
+// One launch, for at most kThreads * kEntries segments and sequences.  In a graph 4.6 us for 64 sequences of a token, 9.1 for 2048
+// segments of 400 000 tokens and 10.7 for 2200 (eight entries a thread, not four); bound by the chain of reads, sum and search, not by the 5 MB.  At 4096
+// segments 9 to 12 us by the number of tokens; the two launches take 20 to 27 at 4097, 56 at 20 000, 0.21 ms at 100 000 and 2.1 ms at 2^20.
 template <int kEntries>
 __global__ __launch_bounds__(kThreads) void place_listed(SegmentList L)
 {
@@ -431,8 +431,8 @@ __global__ __launch_bounds__(kThreads) void place_slots(prep_block_args A, Block
     }
 }
 
-// One launch, for at most kThreads * kEntries requests.  In a graph 3.5 us for 128 requests of a token, 10 for 2000 of 300 000 tokens.  At 4096
-// requests 13 to 15 us; the two launches take 20 to 30 at 4097.
+// One launch, for at most kThreads * kEntries requests.  In a graph 4.1 us for 128 requests of a token, 10 for 2000 of 300 000 tokens.  At 4096
+// requests 14 to 16 us by the number of tokens; the two launches take 20 to 32 at 4097, 71 to 90 at 20 000, 0.34 to 0.38 ms at 100 000 and 3.5 to 3.9 ms at 2^20.
 template <int kEntries>
 __global__ __launch_bounds__(kThreads) void place_slots_listed(prep_block_args A, BlockSize B)
 {

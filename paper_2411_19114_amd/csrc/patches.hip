@@ -10,8 +10,8 @@
 // took as long as the rest of the kernel.  The sums over columns are vector instructions, a lane an output column whose weights stay in registers.
 // The values go to LDS in the order of the patch rows, from where they are written in runs.
 //
-// Measured, us: 48 frames of 1920 x 1080 to 400 000 pixels, bf16, antialiased 190 (their bytes at 5.2 TB/s: 78; a thread a
-// pixel, patch_rows_direct, 552); 64 frames of some 560 x 420, two taps, fp32 72 (30; 124); 32 photographs, fp16 29 (9.5; 72).  Neither unit is
+// Measured, us a pass among passes over other data: 48 frames of 1920 x 1080 to 400 000 pixels, bf16, antialiased 191 (their bytes at 5.2 TB/s: 78; a thread a
+// pixel, patch_rows_direct, 519); 64 frames of some 560 x 420, two taps, fp32 75 (30; 94); 32 photographs, fp16 27 (9.5; 59).  Neither unit is
 // full: in the first the vector ALU is busy 45 % of the time, LDS 45 %, and waves wait 53 % of theirs.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -47,7 +47,7 @@ __host__ __device__ __forceinline__ Divisor divisor(int d) { return {(uint32_t)d
 
 // A tile's limits, for clips whose windows hold at most kFewTaps columns (kWide = false) and for the others.
 constexpr int kTileCols = 64, kTileRows = 16, kPatches = 128;
-constexpr int kStrip = 4;                          // tiles one below the other that a workgroup takes, at most (2: 205 us for 196, 84 for 75)
+constexpr int kStrip = 4;                          // tiles one below the other that a workgroup takes, at most (2: 201 us for 191, 85 for 75)
 constexpr int kNarrowest = 6;                      // narrowest image whose rows hold a read of 16 bytes
 constexpr int kFewTaps = 3, kMostTaps = 6;          // columns of a window whose weights stay in registers
 constexpr int kSomeTaps = 5;                       // fewer than kMostTaps, where a window has no more
@@ -654,7 +654,7 @@ enum { kDirect = 0, kNarrow = 1, kWide = 2, kKinds = 3 };
 // launch and in two, antialiased, fp16: photographs of 400 x 365 with one picture of 4000 x 3000 reduced to 2^20 pixels, 4 of them 54 and 59, 16 of them 61 and
 // 62, 32 of them 76 and 72, 128 of them 180 and 132; frames of 380 x 285 up to 520 x 390 reduced to 147 456 pixels where they have more, 96 of them
 // 106 and 90, 256 of them 263 and 193; two taps, fp32, of 300 x 225 up to 900 x 675, 64 of them 77 and 84, 96 of them 125 and 114.
-// Threads of a workgroup, 256 and 512, us: narrow 28.5 and 41 (32 photographs), wide 266 and 196 (48 full-HD frames).
+// Threads of a workgroup, 256 and 512, us: narrow 29 and 36 (32 photographs), wide 260 and 191 (48 full-HD frames).
 constexpr uint64_t kOwnLaunchPixels = 1 << 22;
 template <int kElement>
 void cut_clips(PatchClip *clips, uint8_t *kinds, int32_t n, const PatchGeometry &g, int64_t out_stride)

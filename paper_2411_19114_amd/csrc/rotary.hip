@@ -139,7 +139,7 @@ union Vec {
     T v[16 / sizeof(T)];
 };
 
-// 16 bytes; kStream: which nobody reads again before the caches have seen as much as they hold.
+// 16 bytes; kStream: past the caches (launch_rows has the rule).
 template <bool kStream>
 __device__ __forceinline__ uint4 load16(const void *p)
 {
@@ -157,8 +157,8 @@ __device__ __forceinline__ void store16(void *p, uint4 v)
     else *static_cast<uint4 *>(p) = v;
 }
 
-// Bound by memory: 30 us for 8192 tokens of 28 + 4 heads of 128 in bf16 with the store into the cache (5.0 TB/s), 43 for 19321 of 16 + 16 heads
-// of 80 in fp16 (4.6), 58 for 16384 of 32 + 8 heads of 64 in fp32, backwards (5.8, part of it from the last-level cache); a thread a pair took 166, 191 and 147.
+// Bound by memory: 29 us for 8192 tokens of 28 + 4 heads of 128 in bf16 with the store into the cache (5.2 TB/s), 42 for 19321 of 16 + 16 heads
+// of 80 in fp16 (4.7), 58 for 16384 of 32 + 8 heads of 64 in fp32, backwards (5.8, part of it from the last-level cache); a thread a pair takes 166, 191 and 146.
 template <typename T, bool kHalves, int kRows, bool kStream>
 __global__ __launch_bounds__(kThreads) void rotary_rows(prep_rotary_args A, RowShape S, const uint64_t *__restrict__ turns)
 {
@@ -319,6 +319,8 @@ int launch_rows(const prep_rotary &R, const prep_rotary_args &A, hipStream_t str
     if (blocks > 0x7FFFFFFF) return PREP_E_TOO_LARGE;
     // Past the caches where what a load takes of a row is whole 128-byte lines: then 34 -> 30 us and 64 -> 58 us (the first and the last
     // of the calls above), 35 -> 29 for rows of 256 in bf16; pieces of 64 bytes 34 -> 34, of 80 and 96 bytes 44 -> 55 and 35 -> 39.
+    // Who reads the outputs at once does not lose by it: with a copy of q and of the caches behind the first call both take 73.5 -> 72, with one of the
+    // outputs behind the last 143 -> 129, the copies alone 43 and 71.
     const bool lines = S.units * 16 % 128 == 0 && rows_aligned(R, A, 128);
     in_launches((uint32_t)blocks, kThreads, [&](uint32_t first, uint32_t n) {
         const dim3 grid(n);
