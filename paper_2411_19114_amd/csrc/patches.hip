@@ -742,13 +742,14 @@ int launch_patch_rows(const uint8_t *rgb, PatchClip *clips, uint8_t *kinds, int3
     uint64_t tiles = 0;
     for (int32_t i = 0; i < n; i++) {
         PatchClip &c = clips[i];
-        any[kinds[i]] = true;
         if (kinds[i] != kDirect) tiles += groups_of(c, g) * (uint64_t)c.tiles_x() * (uint64_t)c.tiles_y();
     }
     // a workgroup takes a strip of tiles where there are plenty, so that it can read one while it works on another
     g.strip = (int)(tiles / 1536 < 1 ? 1 : tiles / 1536 > kStrip ? kStrip : tiles / 1536);
     for (int32_t i = 0; i < n; i++) {
         PatchClip &c = clips[i];
+        if (kinds[i] != kDirect && blocks_of(c, g, kinds[i]) > 0x7FFFFFFFull) kinds[i] = kDirect;  // (which add() has bounded)
+        any[kinds[i]] = true;
         if (kinds[i] == kDirect) continue;
         c.strips_x_m = divisor(c.tiles_x()).m;
         c.strips_m = divisor(strips_of(c, g)).m;

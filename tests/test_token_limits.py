@@ -266,3 +266,17 @@ def test_large_pictures_among_photographs(patches, photographs, large, threads):
     rc = patches.lib.prep_patch_rows(0, C.c_void_p(4096), prep._packed("Q", [0] * n), prep._packed("i", [w for w, _ in sizes]), prep._packed("i", [h for _, h in sizes]),
                                      prep._packed("i", [3 * w for w, _ in sizes]), None, None, n, C.byref(params), C.c_void_p(4096), C.c_int64(0), C.c_int64(2 ** 30), starts, None)
     assert rc == 0 and [t for _, _, t in patches.launches()] == threads
+
+
+def test_more_tiles_than_a_launch_counts(patches):
+    """A frame of a column of 80 pixels has two strips of tiles: 2^31 - 1 frames have more of them than 32 bits count, and go pixel by pixel."""
+    frames, w, h = 2 ** 31 - 1, 6, 480
+    params = prep.make_patch_params(1, 1, 1, "bf16", cases.MEAN, cases.STD, prep.FILTER_ANTIALIAS, max_pixels=80)
+    assert prep.patch_grid(params, w, h, frames) == (frames, 80, 1)
+    starts = (C.c_int64 * 2)()
+    patches.want()
+    rc = patches.lib.prep_patch_rows(0, C.c_void_p(4096), prep._packed("Q", [0]), prep._packed("i", [w]), prep._packed("i", [h]), prep._packed("i", [3 * w]),
+                                     prep._packed("i", [frames]), prep._packed("Q", [3 * w * h]), 1, C.byref(params), C.c_void_p(4096), C.c_int64(0),
+                                     C.c_int64(2 ** 50), starts, None)
+    assert rc == 0 and list(starts) == [0, 80 * frames]
+    assert in_launches_that_fit(patches.launches()) == -(-80 * frames // 256)
