@@ -630,7 +630,7 @@ def check_slow_pairs(backend, adjacent=False):
 
 # (a launch takes 64 clips of a kind; those narrower than 6 pixels are of a kind of their own)
 PATCHES_MORE = {
-    "several_launches": ([(4 + i % 5, 4 + i % 3) for i in range(330)], [1] * 330, 4, 1, 1, "f16", True, 0, 0),
+    "several_launches": ([(4 + i % 5, 4 + i % 3) for i in range(170)], [1] * 170, 4, 1, 1, "f16", True, 0, 0),
     # reductions of both axes by 2.25, 2.5, 2.81, 3 and 3.21: windows of 5, 6, 6, 7 and 7 samples
     "window_of_five": ([(225, 45)], [1], 2, 1, 1, "f32", True, 0, 100 * 20),
     "window_of_six_least": ([(225, 45), (45, 110)], [1, 1], 2, 1, 1, "f32", True, 0, 90 * 18),
