@@ -473,7 +473,7 @@ int prep_patch_grid(const prep_patch_params *params, int32_t width, int32_t heig
  *            what lies between rows and behind the last one is left as it was
  *   row_starts  HOST, n + 1 entries, written by the call: clip i has rows row_starts[i] up to
  *            row_starts[i + 1].  PREP_E_TOO_LARGE, and nothing enqueued, if out_rows is fewer.
- * PREP_E_INVALID_ARG for a clip of 2^39 output pixels or more, the last group's repeated frames among them.
+ * PREP_E_INVALID_ARG for a clip of more than 2^39 - 256 output pixels, the last group's repeated frames among them.
  */
 int prep_patch_rows(int32_t device, const uint8_t *rgb, const uint64_t *rgb_offsets, const int32_t *widths,
                     const int32_t *heights, const int32_t *pitches, const int32_t *frames,
